@@ -31,7 +31,11 @@ EXPORTS = ["xgen_patconv_pack", "xgen_patconv_run", "xgen_patconv_run_static_scr
            "xgen_patconv_launch_count", "xgen_patconv_probe", "xgen_patconv_run_fused",
            "xgen_blockgemm_pack", "xgen_blockgemm_run", "xgen_blockgemm_query", "xgen_blockgemm_view",
            "xgen_blockgemm_free", "xgen_blockgemm_last_status", "xgen_blockgemm_test_expect_arrivals",
-           "xgen_dwconv_pack", "xgen_dwconv_run", "xgen_dwconv_query", "xgen_dwconv_free"]
+           "xgen_dwconv_pack", "xgen_dwconv_run", "xgen_dwconv_query", "xgen_dwconv_free",
+           "xgen_adapters_pack", "xgen_adapters_run", "xgen_adapters_last_status", "xgen_adapters_free",
+           "xgen_attention_pack", "xgen_attention_append", "xgen_attention_read", "xgen_attention_workspace",
+           "xgen_attention_run", "xgen_attention_last_status", "xgen_attention_free",
+           "xgen_logprobs_pack", "xgen_logprobs_run", "xgen_logprobs_free"]
 
 
 class Desc(ctypes.Structure):
@@ -113,6 +117,32 @@ class GemmHostView(ctypes.Structure):
     _fields_ = [("units", ctypes.c_void_p), ("n_units", ctypes.c_int64), ("seg_off", ctypes.c_void_p)]
 
 
+class AdaptersDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int32), ("c_out", ctypes.c_int32), ("rank", ctypes.c_int32), ("adapters", ctypes.c_int32),
+                ("dtype", ctypes.c_int)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("dtype", ctypes.c_int), ("rotary", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("window", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class AttentionBatch(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int32), ("longest", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("row_start_dev", ctypes.c_void_p), ("length_dev", ctypes.c_void_p), ("page_table_dev", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64)]
+
+
+class AttentionCache(ctypes.Structure):
+    _fields_ = [("k_codes_dev", ctypes.c_void_p), ("v_codes_dev", ctypes.c_void_p), ("k_scale_dev", ctypes.c_void_p),
+                ("v_scale_dev", ctypes.c_void_p), ("pages", ctypes.c_int64)]
+
+
+class LogProbsDesc(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("top", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
 class HostView(ctypes.Structure):
     _fields_ = [("slots", ctypes.c_void_p), ("n_slots", ctypes.c_int64),
                 ("seg_off", ctypes.c_void_p), ("slot_oc", ctypes.c_void_p),
@@ -135,7 +165,8 @@ def _bind_calls(L):
     m = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(m)
     m.bind(*(ctypes.cast(getattr(L, "xgen_" + f), ctypes.c_void_p).value
-             for f in ("patconv_run", "patconv_run_fused", "blockgemm_run", "dwconv_run")))
+             for f in ("patconv_run", "patconv_run_fused", "blockgemm_run", "dwconv_run", "adapters_run", "logprobs_run",
+                       "attention_append", "attention_read", "attention_run")))
     return m
 
 
@@ -181,9 +212,24 @@ def lib():
         L.xgen_dwconv_query.argtypes = [P, ctypes.POINTER(ctypes.c_int64)]
         L.xgen_dwconv_free.argtypes = [P]
         L.xgen_dwconv_free.restype = None
+        J = ctypes.c_int64
+        L.xgen_adapters_pack.argtypes = [ctypes.POINTER(AdaptersDesc), P, P, P, ctypes.c_int, ctypes.POINTER(P)]
+        L.xgen_adapters_run.argtypes = [P, P, J, J, P, P, J, P, J, P, J, P]
+        L.xgen_adapters_last_status.argtypes = [P, P]
+        L.xgen_attention_pack.argtypes = [ctypes.POINTER(AttentionDesc), P, ctypes.c_int, ctypes.POINTER(P)]
+        L.xgen_attention_append.argtypes = [P, P, P, J, ctypes.POINTER(AttentionBatch), ctypes.POINTER(AttentionCache), P]
+        L.xgen_attention_read.argtypes = [P, ctypes.POINTER(AttentionBatch), ctypes.POINTER(AttentionCache), ctypes.c_int, P, P, J, P]
+        L.xgen_attention_workspace.argtypes = [P, ctypes.POINTER(AttentionBatch), ctypes.POINTER(J)]
+        L.xgen_attention_run.argtypes = [P, P, J, ctypes.POINTER(AttentionBatch), ctypes.POINTER(AttentionCache), P, J, P, P]
+        L.xgen_attention_last_status.argtypes = [P, P]
+        L.xgen_logprobs_pack.argtypes = [ctypes.POINTER(LogProbsDesc), ctypes.c_int, ctypes.POINTER(P)]
+        L.xgen_logprobs_run.argtypes = [P, P, J, J, P, P, P, P, P, P]
+        for name in ("adapters", "attention", "logprobs"):
+            free = getattr(L, "xgen_%s_free" % name)
+            free.argtypes, free.restype = [P], None
         for name in EXPORTS:
             if name not in ("xgen_patconv_free", "xgen_strerror", "xgen_patconv_launch_count", "xgen_blockgemm_free",
-                            "xgen_dwconv_free"):
+                            "xgen_dwconv_free", "xgen_adapters_free", "xgen_attention_free", "xgen_logprobs_free"):
                 getattr(L, name).restype = ctypes.c_int
         _calls = _bind_calls(L)
         _lib = L
@@ -438,3 +484,143 @@ class Depthwise:
         status = _calls.dw(self._h.value, x_ptr, n, h, w, bias_ptr, relu, y_ptr, stream)
         if status:
             raise PatconvError(status, "xgen_dwconv_run")
+
+
+class _Handle:
+    """Owner of one handle; `_free` names the library's call that releases it."""
+
+    _free = ""
+
+    def __init__(self):
+        self._h = ctypes.c_void_p()
+
+    def close(self):
+        if self._h:
+            getattr(lib(), self._free)(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Adapters(_Handle):
+    """Owner of one xgen_adapters_packed handle: low-rank adapters of many requests beside a shared product.
+
+    a [adapters, rank, k], b [adapters, c_out, rank] in the layer's type, scale [adapters] (1 where None)."""
+
+    _free = "xgen_adapters_free"
+
+    def __init__(self, k, c_out, dtype, a, b, scale=None, device=0):
+        super().__init__()
+        self.dtype = DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+        self.k, self.c_out = int(k), int(c_out)
+        want = {F32: np.float32, F16_F32ACC: np.float16}.get(self.dtype, np.float32)
+        a, b = np.ascontiguousarray(a, dtype=want), np.ascontiguousarray(b, dtype=want)
+        if a.ndim != 3 or b.ndim != 3 or a.shape[2] != k or b.shape[1] != c_out or a.shape[:2] != (b.shape[0], b.shape[2]):
+            raise ValueError("a must be [adapters,rank,k] and b [adapters,c_out,rank]")
+        self.adapters, self.rank = a.shape[:2]
+        s = np.ones(self.adapters, np.float32) if scale is None else np.ascontiguousarray(scale, dtype=np.float32)
+        if s.shape != (self.adapters,):
+            raise ValueError("scale must be [adapters]")
+        d = AdaptersDesc(self.k, self.c_out, self.rank, self.adapters, self.dtype)
+        _check(lib().xgen_adapters_pack(ctypes.byref(d), a.ctypes.data, b.ctypes.data, s.ctypes.data, int(device),
+                                        ctypes.byref(self._h)), "xgen_adapters_pack")
+
+    def run(self, x_ptr, rows, x_stride, row_start_ptr, adapter_ptr, requests, y_ptr, y_stride, out_ptr, out_stride, stream=0):
+        """Enqueue out = y + what the requests' adapters add (out_ptr may be y_ptr); device addresses as ints, strides in elements."""
+        status = _calls.adapters(self._h.value, x_ptr, rows, x_stride, row_start_ptr, adapter_ptr, requests, y_ptr, y_stride, out_ptr,
+                                 out_stride, stream)
+        if status:
+            raise PatconvError(status, "xgen_adapters_run")
+
+    def sync(self, stream=0):
+        _check(lib().xgen_adapters_last_status(self._h, stream or None), "xgen_adapters_last_status")
+
+
+class Cache:
+    """The paged key/value cache's device memory, as the attention calls take it (xgen_attention_cache)."""
+
+    def __init__(self, k_codes_ptr, v_codes_ptr, k_scale_ptr, v_scale_ptr, pages):
+        self._c = AttentionCache(k_codes_ptr, v_codes_ptr, k_scale_ptr, v_scale_ptr, int(pages))
+        self.address = ctypes.addressof(self._c)
+
+
+class Batch:
+    """The sequences of one call (xgen_attention_batch); device addresses as ints.  Lengths, row starts and the page
+    table are read by the kernels, so one Batch serves as long as their addresses and the sizes named here hold."""
+
+    def __init__(self, sequences, rows, longest, row_start_ptr, length_ptr, page_table_ptr, table_stride):
+        self._b = AttentionBatch(int(sequences), int(longest), int(rows), row_start_ptr, length_ptr, page_table_ptr, int(table_stride))
+        self.address = ctypes.addressof(self._b)
+
+
+class Attention(_Handle):
+    """Owner of one xgen_attention_packed handle: appending to a paged cache of 8 bits, reading it back, attention over it.
+
+    freq: radians per position of each turned pair (float64), or None for no rotation."""
+
+    _free = "xgen_attention_free"
+
+    def __init__(self, q_heads, kv_heads, head_dim, page_tokens, dtype, freq=None, interleaved=False, window=0, softmax_scale=0.0,
+                 device=0):
+        super().__init__()
+        self.dtype = DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+        f = None if freq is None or len(freq) == 0 else np.ascontiguousarray(freq, dtype=np.float64)
+        if f is not None and f.ndim != 1:
+            raise ValueError("freq must be [rotary/2]")
+        d = AttentionDesc(int(q_heads), int(kv_heads), int(head_dim), int(page_tokens), self.dtype, 0 if f is None else 2 * len(f),
+                          int(bool(interleaved)), int(window), float(softmax_scale))
+        _check(lib().xgen_attention_pack(ctypes.byref(d), None if f is None else f.ctypes.data, int(device), ctypes.byref(self._h)),
+               "xgen_attention_pack")
+
+    def append(self, k_ptr, v_ptr, kv_stride, batch, cache, stream=0):
+        """Enqueue: the batch's new keys (turned) and values into the cache."""
+        status = _calls.append(self._h.value, k_ptr, v_ptr, kv_stride, batch.address, cache.address, stream)
+        if status:
+            raise PatconvError(status, "xgen_attention_append")
+
+    def read(self, batch, cache, k_ptr, v_ptr, stride, dtype, stream=0):
+        """Enqueue: what the cache holds of the batch's rows, as dtype ("f32" or "f16")."""
+        status = _calls.read(self._h.value, batch.address, cache.address, DTYPES[dtype] if isinstance(dtype, str) else int(dtype), k_ptr,
+                             v_ptr, stride, stream)
+        if status:
+            raise PatconvError(status, "xgen_attention_read")
+
+    def workspace(self, batch) -> int:
+        """Bytes of device memory that run() takes for such a batch."""
+        n = ctypes.c_int64()
+        _check(lib().xgen_attention_workspace(self._h, ctypes.byref(batch._b), ctypes.byref(n)), "xgen_attention_workspace")
+        return n.value
+
+    def run(self, q_ptr, q_stride, batch, cache, y_ptr, y_stride, workspace_ptr, stream=0):
+        """Enqueue attention of the batch's rows over the cache."""
+        status = _calls.attend(self._h.value, q_ptr, q_stride, batch.address, cache.address, y_ptr, y_stride, workspace_ptr, stream)
+        if status:
+            raise PatconvError(status, "xgen_attention_run")
+
+    def sync(self, stream=0):
+        _check(lib().xgen_attention_last_status(self._h, stream or None), "xgen_attention_last_status")
+
+
+class LogProbs(_Handle):
+    """Owner of one xgen_logprobs_packed handle: log probability of given tokens, entropy and top alternatives of rows of logits."""
+
+    _free = "xgen_logprobs_free"
+
+    def __init__(self, vocab, dtype, top=0, device=0):
+        super().__init__()
+        self.dtype = DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+        self.vocab, self.top = int(vocab), int(top)
+        d = LogProbsDesc(self.vocab, self.top, self.dtype)
+        _check(lib().xgen_logprobs_pack(ctypes.byref(d), int(device), ctypes.byref(self._h)), "xgen_logprobs_pack")
+
+    def run(self, x_ptr, rows, row_stride, token_ptr, logprob_ptr, entropy_ptr, top_ptr, top_logprob_ptr, stream=0):
+        """Enqueue; device addresses as ints, 0 for what is not asked for."""
+        if not self.top:
+            top_ptr = top_logprob_ptr = 0
+        status = _calls.logprobs(self._h.value, x_ptr, rows, row_stride, token_ptr, logprob_ptr, entropy_ptr, top_ptr, top_logprob_ptr, stream)
+        if status:
+            raise PatconvError(status, "xgen_logprobs_run")

@@ -12,9 +12,11 @@ _CSRC = os.path.join(_HERE, "csrc")
 _INC = os.path.join(os.path.dirname(_HERE), "include")
 LIB_PATH = os.path.join(_HERE, "libpatconv.so")
 CALLS_PATH = os.path.join(_HERE, "_calls.abi3.so")     # the enqueueing calls for Python
-_SOURCES = ["patconv.cu", "tapgemm.cu", "tapgemm_f32.cu", "tapgemm_f16.cu", "tapgemm_f16_cut.cu", "tapgemm_i8.cu", "fewconv.cu", "blockgemm.cu", "dwconv.cu", "probe.cu", "pack.cpp"]
-_DEPS = _SOURCES + ["patconv_internal.h", "ptx.cuh", "tapgemm.h", "tapgemm_kernel.cuh", "fewconv.h", "gen_core.py", "gen_blockgemm.py", os.path.join(_INC, "patconv.h"),
-                    os.path.join(_INC, "blockgemm.h"), os.path.join(_INC, "dwconv.h")]
+_SOURCES = ["patconv.cu", "tapgemm.cu", "tapgemm_f32.cu", "tapgemm_f16.cu", "tapgemm_f16_cut.cu", "tapgemm_i8.cu", "fewconv.cu", "blockgemm.cu", "dwconv.cu", "probe.cu", "pack.cpp",
+            "adapters.cu", "attention.cu", "logprobs.cu"]
+_DEPS = _SOURCES + ["patconv_internal.h", "ptx.cuh", "serve.cuh", "tapgemm.h", "tapgemm_kernel.cuh", "fewconv.h", "gen_core.py", "gen_blockgemm.py", os.path.join(_INC, "patconv.h"),
+                    os.path.join(_INC, "blockgemm.h"), os.path.join(_INC, "dwconv.h"), os.path.join(_INC, "adapters.h"),
+                    os.path.join(_INC, "attention.h"), os.path.join(_INC, "logprobs.h")]
 
 
 _OBJ_DIR = os.path.join(_HERE, "_build")
@@ -29,6 +31,8 @@ _INCLUDES = {
     "dwconv.cu": ["patconv_internal.h", os.path.join(_INC, "patconv.h"), os.path.join(_INC, "dwconv.h")],
     "probe.cu": [os.path.join(_INC, "patconv.h")],
     "pack.cpp": ["patconv_internal.h", os.path.join(_INC, "patconv.h")],
+    **{name + ".cu": ["patconv_internal.h", "serve.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, name + ".h")]
+       for name in ("adapters", "attention", "logprobs")},
 }
 
 
@@ -41,7 +45,7 @@ def build_calls(force: bool = False) -> str:
     that is there was made from these sources."""
     src = os.path.join(_CSRC, "calls.cpp")
     digest = hashlib.sha256()
-    for f in [src] + [os.path.join(_INC, h) for h in ("patconv.h", "blockgemm.h", "dwconv.h")]:
+    for f in [src] + [os.path.join(_INC, h) for h in ("patconv.h", "blockgemm.h", "dwconv.h", "adapters.h", "attention.h", "logprobs.h")]:
         with open(f, "rb") as fh:
             digest.update(fh.read())
     tag = "sources " + digest.hexdigest()          # stands in the file: a copy of the tree need not keep its times

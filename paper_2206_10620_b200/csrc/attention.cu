@@ -1,0 +1,1048 @@
+// libpatconv: a paged key/value cache of 8 bits and attention over it, for sm_100a, and their C ABI.
+//
+// append  one block per page that new tokens reach, head, and keys or values: the new entries go through shared memory in
+//         fp32 (turned there, if keys), their largest magnitude decides the page's scale, codes leave 16 bytes at a time.
+// read    codes times scales, 16 codes a thread.
+// run     `narrow_kernel`: few query rows (up to 16 with all query heads of a key head) against the whole cache of a sequence, bound
+//         by the cache's bytes.  The work of a call is a line of units (64 tokens of one key head, for one tile of rows), cut into
+//         equal pieces, one for each block that the GPU holds at once; where a cut falls inside a tile's tokens the pieces
+//         leave partial results, which `combine_kernel` joins in their order.  So any mixture of lengths fills the GPU evenly.
+//
+// A code is an integer of at most 127, exact in fp16: the matrix instructions take codes widened to fp16 (by byte permutes
+// and one subtraction), the page's scales are applied to scores and probabilities in fp32.
+#include <cmath>
+#include <climits>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "attention.h"
+#include "serve.cuh"
+
+struct xgen_attention_packed {
+    xgen_attention_desc d;
+    int device, sms;
+    int workers;                // blocks of narrow_kernel that the device holds at once
+    uint64_t *d_freq;           // [rotary/2] turns per position, as 64-bit fractions
+    int *d_status;
+};
+
+namespace attention {
+using namespace serve;
+
+// The batch and the cache as the kernels see them.
+struct Batch {
+    const int32_t *row_start, *length, *table;
+    int64_t table_stride;
+    int sequences, rows, longest;
+};
+struct Cache {
+    int8_t *codes[2];           // keys, values
+    float *scale[2];
+    int64_t pages;
+    int heads, page_tokens;
+};
+struct Rotation {
+    const uint64_t *freq;
+    int rotary, interleaved;
+};
+
+constexpr int kLongest = 1 << 30;    // tokens of a sequence
+__device__ __forceinline__ int length_of(const Batch &B, int s) { return min(max(B.length[s], 0), kLongest); }
+// First row and number of rows of a sequence.
+struct Span { int row, n; };
+__device__ __forceinline__ Span span_of(const Batch &B, int s) {
+    const int lo = min(max(B.row_start[s], 0), B.rows);
+    return {lo, max(min(B.row_start[s + 1], B.rows) - lo, 0)};
+}
+// The page of a token, or -1.
+__device__ __forceinline__ int64_t page_of(const Batch &B, const Cache &C, int s, int token) {
+    const int at = token / C.page_tokens;
+    if (at >= B.table_stride) return -1;
+    const int p = B.table[(int64_t)s * B.table_stride + at];
+    return p >= 0 && p < C.pages ? p : -1;
+}
+// Components of pair u of a head of `dim`: those behind the turned ones pair up too, for convenience.
+__device__ __forceinline__ int2 pair_of(const Rotation &R, int u) {
+    if (u >= R.rotary / 2 || R.interleaved) return make_int2(2 * u, 2 * u + 1);
+    return make_int2(u, u + R.rotary / 2);
+}
+__device__ __forceinline__ void turn(const Rotation &R, int u, int position, float &a, float &b) {
+    // position times the frequency in turns, modulo one turn: the upper half of a 64-bit product that wraps
+    const int32_t frac = (int32_t)((R.freq[u] * (uint64_t)position) >> 32);
+    float s, c;
+    sincospif((float)frac * 4.6566128730773926e-10f, &s, &c);        // 2^-31: half turns
+    const float x = a * c - b * s, y = a * s + b * c;
+    a = x;
+    b = y;
+}
+
+// ---- append ------------------------------------------------------------------------------------------------------------------
+struct AppendParams {
+    Batch batch;
+    Cache cache;
+    Rotation rotation;
+    const void *in[2];
+    int64_t stride;
+    int dim, room;              // room: tokens that the shared memory holds
+    bool vec[2];
+    int *status;
+};
+
+constexpr int kAppendThreads = 128;
+
+template <int DT> __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams P) {
+    using T = typename Elem<DT>::T;
+    extern __shared__ __align__(16) float entries[];     // [new tokens of the page][dim]
+    __shared__ unsigned most_bits[kAppendThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int which = blockIdx.z, head = blockIdx.y, H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens;
+    const bool keys = which == 0;
+    wait_before();
+
+    // the page: number `want` of those that the batch's new tokens reach
+    int seq = -1, page_at = 0;
+    {
+        int64_t before = 0;
+        const int want = blockIdx.x;
+        for (int i0 = 0; i0 < P.batch.sequences; i0 += 32) {
+            const int i = i0 + lane;
+            int first = 0, count = 0;
+            if (i < P.batch.sequences) {
+                const int n = span_of(P.batch, i).n, length = length_of(P.batch, i);
+                const int p0 = max(length - n, 0);
+                if (n > 0 && length > p0) { first = p0 / PT; count = (length - 1) / PT - first + 1; }
+            }
+            int upto = count;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(~0u, upto, d);
+                if (lane >= d) upto += v;
+            }
+            const unsigned hit = __ballot_sync(~0u, want < before + upto);
+            if (hit) {
+                const int at = __ffs(hit) - 1;
+                seq = i0 + at;
+                page_at = __shfl_sync(~0u, first, at) + (int)(want - before) - (__shfl_sync(~0u, upto, at) - __shfl_sync(~0u, count, at));
+                break;
+            }
+            before += __shfl_sync(~0u, upto, 31);
+        }
+    }
+    if (seq < 0) return;
+    const Span sp = span_of(P.batch, seq);
+    const int length = length_of(P.batch, seq);
+    const int lo = max(max(length - sp.n, 0), page_at * PT);
+    const int hi = (int)min((int64_t)length, (int64_t)(page_at + 1) * PT);
+    const int n = hi - lo, slot = lo - page_at * PT;
+    const int64_t page = page_of(P.batch, P.cache, seq, lo);
+    if (page < 0 || n > P.room) {
+        if (tid == 0) atomicExch(P.status, 1);
+        return;
+    }
+    const T *const in = static_cast<const T *>(P.in[which]) + (int64_t)(sp.row + (lo - (length - sp.n))) * P.stride + (int64_t)head * D;
+
+    // ---- the new entries, in fp32
+    const int pieces = n * (D / 8);
+    for (int c = tid; c < pieces; c += kAppendThreads) {
+        const int token = c / (D / 8), at = c % (D / 8) * 8;
+        const T *const from = in + (int64_t)token * P.stride + at;
+        T v[8];
+        if (P.vec[which]) {
+            uint4 raw[sizeof(T) / 2];
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = __ldg(reinterpret_cast<const uint4 *>(from) + i);
+            memcpy(v, raw, sizeof v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = from[i];
+        }
+        float *const to = entries + token * D + at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[i] = widen(v[i]);
+    }
+    __syncthreads();
+    if (keys && P.rotation.rotary) {
+        const int pairs = P.rotation.rotary / 2;
+        for (int c = tid; c < n * pairs; c += kAppendThreads) {
+            const int token = c / pairs, u = c % pairs;
+            const int2 at = pair_of(P.rotation, u);
+            float *const e = entries + token * D;
+            float a = e[at.x], b = e[at.y];
+            turn(P.rotation, u, lo + token, a, b);
+            e[at.x] = a;
+            e[at.y] = b;
+        }
+        __syncthreads();
+    }
+    unsigned most = 0;                                    // the largest magnitude, as bits: a NaN is above infinity
+    for (int c = tid; c < n * D; c += kAppendThreads) most = max(most, __float_as_uint(entries[c]) & 0x7FFFFFFFu);
+    most = __reduce_max_sync(~0u, most);
+    if (lane == 0) most_bits[warp] = most;
+    float *const scale_at = P.cache.scale[which] + page * H + head;
+    const float was = slot ? *scale_at : 0.0f;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAppendThreads / 32; ++i) most = max(most, most_bits[i]);
+    const float amax = __uint_as_float(most);
+
+    // ---- the scale
+    float scale = was;
+    int halvings = 0;
+    if (most >= 0x7F800000u || isnan(was)) scale = NAN;
+    else if (!(was > 0.0f)) {
+        scale = most ? fmaxf(amax / 127.0f, 1.17549435e-38f) : 0.0f;
+        halvings = 100;                                   // older entries are 0
+    } else
+        while (amax > 127.5f * scale) { scale *= 2.0f; ++halvings; }
+    if (tid == 0) *scale_at = scale;
+
+    // ---- codes
+    int8_t *const codes = P.cache.codes[which] + (page * H + head) * (int64_t)PT * D;
+    if (halvings > 0) {
+        const float by = pow2(-min(halvings, 100));
+        for (int c = tid; c < slot * (D / 16); c += kAppendThreads) {
+            uint4 raw = reinterpret_cast<const uint4 *>(codes)[c];
+            int8_t q[16];
+            memcpy(q, &raw, 16);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) q[i] = (int8_t)__float2int_rn((float)q[i] * by);
+            memcpy(&raw, q, 16);
+            reinterpret_cast<uint4 *>(codes)[c] = raw;
+        }
+    }
+    const float by = scale > 0.0f ? 1.0f / scale : 0.0f;   // (0 for a NaN too: the codes are 0 then)
+    for (int c = tid; c < n * (D / 16); c += kAppendThreads) {
+        const float *const e = entries + c * 16;
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int q = by > 0.0f ? min(max(__float2int_rn(e[4 * i + j] * by), -127), 127) : 0;
+                w[i] |= (uint32_t)(q & 255) << (8 * j);
+            }
+        }
+        reinterpret_cast<uint4 *>(codes + (int64_t)slot * D)[c] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// ---- read --------------------------------------------------------------------------------------------------------------------
+struct ReadParams {
+    Batch batch;
+    Cache cache;
+    void *out[2];
+    int64_t stride;
+    int dim;
+    bool vec[2];
+    int *status;
+};
+
+constexpr int kReadThreads = 256;
+
+template <int DT> __global__ void __launch_bounds__(kReadThreads) read_kernel(const ReadParams P) {
+    using T = typename Elem<DT>::T;
+    const int which = blockIdx.y, H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens;
+    const int per_row = H * D / 16;
+    wait_before();
+    const int64_t i = (int64_t)blockIdx.x * kReadThreads + threadIdx.x;
+    const int64_t row = i / per_row;
+    if (row >= P.batch.rows) return;
+    const int head = (int)(i % per_row) / (D / 16), at = (int)(i % per_row) % (D / 16) * 16;
+    int lo = 0, hi = P.batch.sequences;                   // the first sequence that ends behind the row
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (P.batch.row_start[mid + 1] > row) hi = mid; else lo = mid + 1;
+    }
+    if (lo >= P.batch.sequences) return;
+    const Span sp = span_of(P.batch, lo);
+    if (row < sp.row) return;
+    const int64_t position = (int64_t)length_of(P.batch, lo) - (sp.row + sp.n - row);
+    if (position < 0) return;
+    const int64_t page = page_of(P.batch, P.cache, lo, (int)position);
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    float scale = 0.0f;
+    if (page < 0) atomicExch(P.status, 1);
+    else {
+        scale = P.cache.scale[which][page * H + head];
+        raw = *reinterpret_cast<const uint4 *>(P.cache.codes[which] + ((page * H + head) * (int64_t)PT + position % PT) * D + at);
+    }
+    int8_t q[16];
+    memcpy(q, &raw, 16);
+    T v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = narrow<T>((float)q[j] * scale);
+    T *const to = static_cast<T *>(P.out[which]) + row * P.stride + head * D + at;
+    if (P.vec[which]) {
+        uint4 w[sizeof(T)];
+        memcpy(w, v, sizeof v);
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T); ++j) reinterpret_cast<uint4 *>(to)[j] = w[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) to[j] = v[j];
+    }
+}
+
+// ---- run: few rows against a long cache ------------------------------------------------------------------------------------------
+constexpr int kRows = 16;            // rows of a tile: query rows times the query heads of one key head
+constexpr int kTokens = 16;          // tokens that a warp takes at a time, in one page
+constexpr float kLift = 32768.0f;
+constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = kWarps * kTokens;
+
+struct RunParams {
+    Batch batch;
+    Cache cache;
+    Rotation rotation;
+    const void *q;
+    void *y;
+    int64_t q_stride, y_stride;
+    int group, window;
+    float scale;                     // softmax scale times log2(e)
+    float *partial;                  // [workers][2][kRows][dim] sums
+    float4 *stats;                   // [workers][2][kRows]: maximum, total, unit of the sums
+    int64_t *cut;                    // [workers][4]: sequence, tile of it, first unit of that tile, its units; behind them the length of a piece
+    int workers;
+    int *status;
+};
+
+// What a sequence asks for: rows, tiles of rows for each key head, units of a tile, where its tokens begin.
+struct Sequence {
+    int row, n, length, from, tiles, units;
+};
+__device__ __forceinline__ Sequence sequence_of(const RunParams &P, int s) {
+    const Span sp = span_of(P.batch, s);
+    Sequence q;
+    q.row = sp.row; q.n = sp.n;
+    // tokens beyond the table's are nobody's
+    const int64_t held = P.batch.table_stride * P.cache.page_tokens;
+    q.length = length_of(P.batch, s);
+    const int end = (int)min((int64_t)q.length, held);
+    if (end < q.length && q.n > 0) atomicExch(P.status, 1);
+    const int first = q.length - q.n;                     // the first row's position (may be negative)
+    q.from = P.window > 0 && first - P.window + 1 > 0 ? (first - P.window + 1) / kTokens * kTokens : 0;
+    q.tiles = (int)(((int64_t)q.n * P.group + kRows - 1) / kRows);
+    q.units = q.n > 0 ? max((end - q.from + kUnit - 1) / kUnit, 1) : 0;
+    return q;
+}
+
+// A place on the line of units: unit `unit` of tile `tile` (of key head `head`) of sequence `s`.
+struct Place {
+    Sequence q;
+    int s, head, tile, unit;
+};
+__device__ __forceinline__ void next_place(const RunParams &P, Place &c) {
+    if (++c.unit < c.q.units) return;
+    c.unit = 0;
+    if (++c.tile < c.q.tiles) return;
+    c.tile = 0;
+    if (++c.head < P.cache.heads) return;
+    c.head = 0;
+    do {
+        if (++c.s >= P.batch.sequences) return;
+        c.q = sequence_of(P, c.s);
+    } while (c.q.n == 0);
+}
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy_async16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t to, const void *from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// Two of the four codes of `r` (its signs flipped: 0 .. 255) as fp16: 1024 + code as bits, less 1152.
+template <int SELECT> __device__ __forceinline__ uint32_t widen_codes(uint32_t flipped) {
+    const uint32_t b = __byte_perm(flipped, 0x64646464u, SELECT);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2 *>(&b), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+template <int DT, int D> struct Narrow {
+    static constexpr bool SPLIT = DT == XGEN_F32;          // operands of 22 bits as two of 11
+    static constexpr bool Q_IN_REGISTERS = !SPLIT && D <= 128;
+    static constexpr int ROW = D + 16;                     // bytes of a token's codes in shared memory: 8 tokens meet no bank twice
+    static constexpr int STAGES = D <= 64 ? 4 : D <= 128 ? 3 : 2;
+    static constexpr int STAGE = 2 * kTokens * ROW;        // keys, values
+    static constexpr int Q_ROW = D + 8;                    // fp16 elements of a query row
+    static constexpr int Q_BYTES = kRows * Q_ROW * 2 * (SPLIT ? 2 : 1);
+    static constexpr int RING = kWarps * STAGES * STAGE;
+    static constexpr int SHARED = RING + Q_BYTES + kRows * D * 4;
+};
+
+template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) narrow_kernel(const RunParams P) {
+    using T = typename Elem<DT>::T;
+    using N = Narrow<DT, D>;
+    extern __shared__ __align__(16) unsigned char shared[];
+    unsigned char *const ring = shared;
+    __half *const qs = reinterpret_cast<__half *>(shared + N::RING);
+    float *const sums = reinterpret_cast<float *>(shared + N::RING + N::Q_BYTES);        // [kRows][D]
+    __shared__ float stage_scale[kWarps][N::STAGES][2];
+    __shared__ float row_factor[kRows];
+    __shared__ float row_most[kWarps][kRows], row_total[kWarps][kRows], warp_unit[kWarps];
+    __shared__ int64_t scan[kWarps + 1], start_units;
+    __shared__ int start_s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int H = P.cache.heads, G = P.group, worker = blockIdx.x;
+    wait_before();
+
+    // ---- this block's piece of the line of units
+    int64_t todo;
+    Place ahead;
+    int64_t skipped;                                       // units of the first tile before the piece
+    {
+        const int each = (P.batch.sequences + kThreads - 1) / kThreads;
+        const int s0 = min(tid * each, P.batch.sequences), s1 = min(s0 + each, P.batch.sequences);
+        int64_t own = 0;
+        for (int s = s0; s < s1; ++s) {
+            const Sequence q = sequence_of(P, s);
+            own += (int64_t)H * q.tiles * q.units;
+        }
+        int64_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t v = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += v;
+        }
+        if (lane == 31) scan[warp + 1] = upto;
+        if (tid == 0) scan[0] = 0;
+        __syncthreads();
+        int64_t before = upto - own, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += scan[w + 1];
+            all += scan[w + 1];
+        }
+        const int64_t piece = max((all + P.workers - 1) / P.workers, (int64_t)1);
+        const int64_t from = piece * worker;
+        todo = min(piece, all - from);
+        if (todo > 0 && before <= from && from < before + own) {
+            int64_t left = from - before;
+            for (int s = s0; s < s1; ++s) {
+                const Sequence q = sequence_of(P, s);
+                const int64_t u = (int64_t)H * q.tiles * q.units;
+                if (left < u) { start_s = s; start_units = left; break; }
+                left -= u;
+            }
+        }
+        __syncthreads();
+        if (todo <= 0) {
+            if (tid == 0) P.cut[worker * 4 + 3] = 0;
+            return;
+        }
+        ahead.s = start_s;
+        ahead.q = sequence_of(P, ahead.s);
+        const int64_t tile = start_units / ahead.q.units;
+        skipped = start_units % ahead.q.units;
+        ahead.unit = (int)skipped;
+        ahead.head = (int)(tile / ahead.q.tiles);
+        ahead.tile = (int)(tile % ahead.q.tiles);
+        if (tid == 0 && worker == 0) P.cut[(int64_t)P.workers * 4] = piece;
+        if (tid == 0) {
+            int64_t *const c = P.cut + worker * 4;
+            c[0] = ahead.s; c[1] = tile; c[2] = from - skipped; c[3] = ahead.q.units;
+        }
+    }
+
+    // ---- tokens on their way: each warp its own
+    const uint32_t my_ring = smem_at(ring) + warp * N::STAGES * N::STAGE;
+    uint32_t there = 0;                                    // bit i: stage i holds a tile of tokens that somebody may see
+    int64_t left_ahead = todo;
+    auto token_of = [&](const Place &c) { return c.q.from + c.unit * kUnit + warp * kTokens; };
+    auto entry_of = [&](const Place &c) {                  // the page table's entry (asked for one unit before it is needed)
+        const int at = token_of(c) / P.cache.page_tokens;
+        return token_of(c) < c.q.length && at < P.batch.table_stride ? P.batch.table[(int64_t)c.s * P.batch.table_stride + at] : -2;
+    };
+    int entry = entry_of(ahead);
+    auto fetch = [&](int stage) {
+        if (left_ahead > 0) {
+            const int token = token_of(ahead);
+            // what the tile's last row sees ends at its own position, what its first row sees begins a window before
+            const int first = ahead.q.length - ahead.q.n + ahead.tile * kRows / G;
+            const int last = min(ahead.q.length - 1, ahead.q.length - ahead.q.n + (ahead.tile * kRows + kRows - 1) / G);
+            const bool seen = token <= last && (P.window == 0 || token + kTokens - 1 > first - P.window);
+            there &= ~(1u << stage);
+            if (entry >= 0 && entry < P.cache.pages) {
+                if (seen) {
+                    const int64_t at = (int64_t)entry * H + ahead.head;
+                    const int64_t from = (at * P.cache.page_tokens + token % P.cache.page_tokens) * D;
+                    const uint32_t to = my_ring + stage * N::STAGE;
+#pragma unroll
+                    for (int i = 0; i < D / 32; ++i) {
+                        const int c = lane + 32 * i, row = c / (D / 16), col = c % (D / 16);
+                        copy_async16(to + row * N::ROW + col * 16, P.cache.codes[0] + from + c * 16);
+                        copy_async16(to + (kTokens + row) * N::ROW + col * 16, P.cache.codes[1] + from + c * 16);
+                    }
+                    if (lane < 2) copy_async4(smem_at(&stage_scale[warp][stage][lane]), P.cache.scale[lane] + at);
+                    there |= 1u << stage;
+                }
+            } else if (entry != -2 && lane == 0) atomicExch(P.status, 1);
+            if (--left_ahead > 0) {
+                next_place(P, ahead);
+                entry = entry_of(ahead);
+            }
+        }
+        copy_async_commit();
+    };
+    Place now = ahead;
+#pragma unroll
+    for (int i = 0; i < N::STAGES - 1; ++i) fetch(i);
+
+    int stage = 0;
+    const uint32_t a_lane = (uint32_t)((lane & 7) + (lane & 8)) * N::ROW + (lane >> 4) * 16;     // this lane's row of four matrices
+    bool whole = skipped == 0;
+    int slot = 0;                                          // of the partial results: 0 for the piece's first tile
+    while (todo > 0) {
+        // ---- one tile of rows: queries, turned, with a power of two for each row that brings them near 2^14
+        const int row0 = now.tile * kRows, rows = min(kRows, now.q.n * G - row0);
+        const int first_position = now.q.length - now.q.n;
+        for (int r = warp; r < kRows; r += kWarps) {
+            float v[D / 32 + 1];
+            unsigned most = 0;
+            const int i = (row0 + r) / G;
+            constexpr int PAIRS = (D / 2 + 31) / 32;
+            const T *const q = static_cast<const T *>(P.q) + (int64_t)(now.q.row + i) * P.q_stride + (int64_t)(now.head * G + (row0 + r) % G) * D;
+#pragma unroll
+            for (int p = 0; p < PAIRS; ++p) {
+                const int u = lane + 32 * p;
+                float a = 0.0f, b = 0.0f;
+                if (r < rows && u < D / 2) {
+                    const int2 at = pair_of(P.rotation, u);
+                    a = widen(q[at.x]);
+                    b = widen(q[at.y]);
+                    if (u < P.rotation.rotary / 2 && first_position + i >= 0) turn(P.rotation, u, first_position + i, a, b);
+                }
+                v[2 * p] = a;
+                v[2 * p + 1] = b;
+                most = max(most, max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu));
+            }
+            most = __reduce_max_sync(~0u, most);
+            const int e = most && most < 0x7F800000u ? max(exponent(__uint_as_float(most)), -100) - 14 : 0;
+            const float by = pow2(-e);
+#pragma unroll
+            for (int p = 0; p < PAIRS; ++p) {
+                const int u = lane + 32 * p;
+                if (u < D / 2) {
+                    const int2 at = pair_of(P.rotation, u);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float x = v[2 * p + j] * by;
+                        const __half hi = __float2half_rn(x);
+                        qs[r * N::Q_ROW + (j ? at.y : at.x)] = hi;
+                        if (N::SPLIT) qs[(kRows + r) * N::Q_ROW + (j ? at.y : at.x)] = __float2half_rn(x - __half2float(hi));
+                    }
+                }
+            }
+            if (lane == 0) row_factor[r] = pow2(e) * P.scale;
+        }
+        __syncthreads();
+        uint2 qf[N::Q_IN_REGISTERS ? D / 16 : 1][2];
+        if (N::Q_IN_REGISTERS) {
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) qf[c][r] = *reinterpret_cast<const uint2 *>(qs + (g + 8 * r) * N::Q_ROW + c * 16 + 4 * t);
+        }
+        float factor[2];
+        int position[2];                                   // of this lane's rows g and g + 8; -1 where there is no row
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            factor[r] = row_factor[g + 8 * r];
+            position[r] = g + 8 * r < rows ? first_position + (row0 + g + 8 * r) / G : -1;
+        }
+        const int least_position = first_position + row0 / G;
+
+        float o[D / 8][4];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, unit = 0.0f;     // unit: the values' scale that o is in
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+
+        // ---- its tokens, as far as the piece goes
+        const int units = (int)min(todo, (int64_t)(now.q.units - now.unit));
+        const bool last_part = now.unit + units == now.q.units;
+        for (int u = 0; u < units; ++u) {
+            fetch(stage == 0 ? N::STAGES - 1 : stage - 1);
+            copy_async_wait<N::STAGES - 1>();
+            __syncwarp();
+            if (there >> stage & 1) {
+                const int token = token_of(now);
+                const uint32_t k_at = my_ring + stage * N::STAGE + a_lane, v_at = k_at + kTokens * N::ROW;
+                const float k_scale = stage_scale[warp][stage][0], v_scale = stage_scale[warp][stage][1];
+                float s[2][4] = {};
+#pragma unroll
+                for (int c = 0; c < D / 16; c += 2) {
+                    uint32_t r[4];
+                    load_matrices(r, k_at + c * 16);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t a[4], low[4];
+                        if (N::Q_IN_REGISTERS) {
+                            a[0] = qf[N::Q_IN_REGISTERS ? c + h : 0][0].x; a[1] = qf[N::Q_IN_REGISTERS ? c + h : 0][1].x;
+                            a[2] = qf[N::Q_IN_REGISTERS ? c + h : 0][0].y; a[3] = qf[N::Q_IN_REGISTERS ? c + h : 0][1].y;
+                        } else {
+                            const uint2 u0 = *reinterpret_cast<const uint2 *>(qs + g * N::Q_ROW + (c + h) * 16 + 4 * t);
+                            const uint2 u1 = *reinterpret_cast<const uint2 *>(qs + (g + 8) * N::Q_ROW + (c + h) * 16 + 4 * t);
+                            a[0] = u0.x; a[1] = u1.x; a[2] = u0.y; a[3] = u1.y;
+                        }
+                        if (N::SPLIT) {
+                            const uint2 u0 = *reinterpret_cast<const uint2 *>(qs + (kRows + g) * N::Q_ROW + (c + h) * 16 + 4 * t);
+                            const uint2 u1 = *reinterpret_cast<const uint2 *>(qs + (kRows + g + 8) * N::Q_ROW + (c + h) * 16 + 4 * t);
+                            low[0] = u0.x; low[1] = u1.x; low[2] = u0.y; low[3] = u1.y;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {      // 8 tokens at a time
+                            const uint32_t f = r[2 * h + e] ^ 0x80808080u, b0 = widen_codes<0x4140>(f), b1 = widen_codes<0x4342>(f);
+                            if (N::SPLIT) mma16(s[e], low, b0, b1);
+                            mma16(s[e], a, b0, b1);
+                        }
+                    }
+                }
+                // scores in powers of two, what a row does not see out of them, the running maximum
+                float most[2] = {-INFINITY, -INFINITY};
+                const bool all_seen = token + kTokens - 1 <= least_position && P.window == 0;       // (what the rows behind the last one see is no matter)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = i >> 1, j = token + 8 * e + 2 * t + (i & 1);
+                        float x = s[e][i] * (k_scale * factor[r]);
+                        if (!all_seen && (j > position[r] || (P.window > 0 && j <= position[r] - P.window))) x = -INFINITY;
+                        s[e][i] = x;
+                        most[r] = x > most[r] || isnan(x) ? x : most[r];
+                    }
+                float alpha[2], base[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                    for (int d = 1; d < 4; d <<= 1) {
+                        const float x = __shfl_xor_sync(~0u, most[r], d);
+                        most[r] = x > most[r] || isnan(x) ? x : most[r];
+                    }
+                    const float now_m = m[r] > most[r] ? m[r] : most[r];
+                    base[r] = now_m == -INFINITY ? 0.0f : now_m;
+                    alpha[r] = exp2_approx(m[r] - base[r]);
+                    m[r] = now_m;
+                }
+                // probabilities times 2^15 (fp16 then holds them down to 2^-29 of the largest), values relative to the largest scale
+                float by = kLift, shrink = 1.0f;
+                if (v_scale > unit && v_scale < INFINITY) {
+                    shrink = unit / v_scale;
+                    unit = v_scale;
+                } else if (unit > 0.0f) by = v_scale < INFINITY ? kLift * (v_scale / unit) : 0.0f;
+                if (!(v_scale < INFINITY)) {               // the rows that see some of the page are lost, the others are not
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        if (!(most[r] == -INFINITY)) l[r] = NAN;
+                }
+                uint32_t p[4], p_low[4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float x0 = exp2_approx(s[e][2 * r] - base[r]), x1 = exp2_approx(s[e][2 * r + 1] - base[r]);
+                        l[r] = e == 0 ? l[r] * alpha[r] + (x0 + x1) : l[r] + (x0 + x1);
+                        p[2 * e + r] = pack_half(x0 * by, x1 * by);
+                        if (N::SPLIT) {
+                            const __half2 h = *reinterpret_cast<const __half2 *>(&p[2 * e + r]);
+                            p_low[2 * e + r] = pack_half(x0 * by - __low2float(h), x1 * by - __high2float(h));
+                        }
+                    }
+                const float f0 = alpha[0] * shrink, f1 = alpha[1] * shrink;
+                if (__any_sync(~0u, f0 != 1.0f || f1 != 1.0f)) {
+#pragma unroll
+                    for (int j = 0; j < D / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+                }
+#pragma unroll
+                for (int c = 0; c < D / 16; c += 2) {
+                    uint32_t r[4];
+                    load_matrices_turned(r, v_at + c * 16);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t x0 = r[2 * h] ^ 0x80808080u, x1 = r[2 * h + 1] ^ 0x80808080u;
+                        const uint32_t even0 = widen_codes<0x4240>(x0), even1 = widen_codes<0x4240>(x1);
+                        const uint32_t odd0 = widen_codes<0x4341>(x0), odd1 = widen_codes<0x4341>(x1);
+                        if (N::SPLIT) {
+                            mma16(o[2 * (c + h)], p_low, even0, even1);
+                            mma16(o[2 * (c + h) + 1], p_low, odd0, odd1);
+                        }
+                        mma16(o[2 * (c + h)], p, even0, even1);
+                        mma16(o[2 * (c + h) + 1], p, odd0, odd1);
+                    }
+                }
+                __syncwarp();                              // the stage is free again
+            }
+            stage = stage + 1 == N::STAGES ? 0 : stage + 1;
+            ++now.unit;
+        }
+        todo -= units;
+
+        // ---- the warps' shares together
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            l[r] += __shfl_xor_sync(~0u, l[r], 1);
+            l[r] += __shfl_xor_sync(~0u, l[r], 2);
+            if (t == 0) { row_most[warp][g + 8 * r] = m[r]; row_total[warp][g + 8 * r] = l[r]; }
+        }
+        if (lane == 0) warp_unit[warp] = unit;
+        __syncthreads();
+        float top[2], total[2], mine[2];
+        float top_unit = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top_unit = warp_unit[w] > top_unit || isnan(warp_unit[w]) ? warp_unit[w] : top_unit;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            top[r] = -INFINITY;
+            total[r] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float x = row_most[w][g + 8 * r];
+                top[r] = x > top[r] || isnan(x) ? x : top[r];
+            }
+            const float base = top[r] == -INFINITY ? 0.0f : top[r];
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) total[r] += row_total[w][g + 8 * r] * exp2_approx(row_most[w][g + 8 * r] - base);
+            mine[r] = unit == 0.0f ? 0.0f : exp2_approx(m[r] - base) * (unit / top_unit);
+        }
+        for (int w = 0; w < kWarps; ++w) {
+            if (warp == w) {
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        float4 *const at = reinterpret_cast<float4 *>(sums + (g + 8 * r) * D + c * 16 + 4 * t);
+                        float4 v = w == 0 ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : *at;
+                        v.x += mine[r] * o[2 * c][2 * r];
+                        v.y += mine[r] * o[2 * c + 1][2 * r];
+                        v.z += mine[r] * o[2 * c][2 * r + 1];
+                        v.w += mine[r] * o[2 * c + 1][2 * r + 1];
+                        *at = v;
+                    }
+            }
+            __syncthreads();
+        }
+        const bool complete = whole && last_part;
+        if (complete) {
+            if (warp == 0 && t == 0) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) row_total[0][g + 8 * r] = total[r] == 0.0f ? 0.0f : top_unit / (total[r] * kLift);
+            }
+            __syncthreads();
+            for (int i = tid; i < rows * D; i += kThreads) {
+                const int r = i / D, row = (row0 + r) / G, head = now.head * G + (row0 + r) % G;
+                const float by = row_total[0][r];
+                static_cast<T *>(P.y)[(int64_t)(now.q.row + row) * P.y_stride + (int64_t)head * D + i % D] = narrow<T>(by == 0.0f ? 0.0f : sums[i] * by);
+            }
+        } else {
+            float *const to = P.partial + ((int64_t)worker * 2 + slot) * kRows * D;
+            for (int i = tid; i < rows * D; i += kThreads) to[i] = sums[i];
+            if (warp == 0 && t == 0) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) P.stats[((int64_t)worker * 2 + slot) * kRows + g + 8 * r] = make_float4(top[r], total[r], top_unit, 0.0f);
+            }
+        }
+        __syncthreads();
+        if (todo > 0) {                                    // on to the next tile of rows
+            --now.unit;
+            next_place(P, now);
+            whole = true;
+            slot = 1;
+        }
+    }
+    copy_async_wait<0>();
+}
+
+// Joins the partial results of the tile that the cut before `worker` falls into, if that is the tile's first cut.
+constexpr int kCombineThreads = 128;
+template <int DT, int D> __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const RunParams P) {
+    using T = typename Elem<DT>::T;
+    const int worker = blockIdx.x + 1, tid = threadIdx.x;
+    wait_before();
+    const int64_t *const cut = P.cut + (int64_t)worker * 4;
+    const int64_t units = cut[3];
+    if (units == 0) return;
+    const int64_t piece = P.cut[(int64_t)P.workers * 4];
+    const int64_t base = cut[2], from = piece * worker;
+    if (base == from || base < from - piece) return;       // the cut is between two tiles, or not the tile's first
+    const int s = (int)cut[0];
+    const Sequence q = sequence_of(P, s);
+    const int head = (int)(cut[1] / q.tiles), tile = (int)(cut[1] % q.tiles);
+    const int row0 = tile * kRows, rows = min(kRows, q.n * P.group - row0);
+    const int last = (int)((base + units - 1) / piece);
+    auto slot_of = [&](int w) { return (int64_t)w * 2 + (base <= piece * w ? 0 : 1); };
+    for (int i = tid; i < rows * (D / 4); i += kCombineThreads) {
+        const int r = i / (D / 4), at = i % (D / 4) * 4;
+        float top = -INFINITY, unit = 0.0f;
+        for (int w = worker - 1; w <= last; ++w) {
+            const float4 x = P.stats[slot_of(w) * kRows + r];
+            top = x.x > top || isnan(x.x) ? x.x : top;
+            unit = fmaxf(unit, x.z);
+        }
+        const float base_m = top == -INFINITY ? 0.0f : top;
+        float total = 0.0f;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int w = worker - 1; w <= last; ++w) {
+            const float4 x = P.stats[slot_of(w) * kRows + r];
+            const float4 o = *reinterpret_cast<const float4 *>(P.partial + (slot_of(w) * kRows + r) * D + at);
+            const float e = exp2_approx(x.x - base_m), f = x.z == 0.0f ? 0.0f : e * (x.z / unit);
+            total += e * x.y;
+            v.x += f * o.x; v.y += f * o.y; v.z += f * o.z; v.w += f * o.w;
+        }
+        const float by = total == 0.0f ? 0.0f : unit / (total * kLift);
+        T *const to = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + r) / P.group) * P.y_stride + (int64_t)(head * P.group + (row0 + r) % P.group) * D + at;
+        const float4 y = by == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
+        to[0] = narrow<T>(y.x); to[1] = narrow<T>(y.y); to[2] = narrow<T>(y.z); to[3] = narrow<T>(y.w);
+    }
+}
+
+// ---- which instance --------------------------------------------------------------------------------------------------------------
+struct Kernels {
+    const void *narrow, *combine;
+    int shared;
+};
+template <int DT, int D> static Kernels kernels_of() {
+    return {(const void *)narrow_kernel<DT, D>, (const void *)combine_kernel<DT, D>, Narrow<DT, D>::SHARED};
+}
+template <int DT> static Kernels kernels_dt(int dim) {
+    switch (dim) {
+    case 32: return kernels_of<DT, 32>();
+    case 64: return kernels_of<DT, 64>();
+    case 96: return kernels_of<DT, 96>();
+    case 128: return kernels_of<DT, 128>();
+    case 192: return kernels_of<DT, 192>();
+    default: return kernels_of<DT, 256>();
+    }
+}
+static Kernels kernels_for(const xgen_attention_desc &d) { return d.dtype == XGEN_F32 ? kernels_dt<XGEN_F32>(d.head_dim) : kernels_dt<XGEN_F16_F32ACC>(d.head_dim); }
+static const void *append_for(xgen_dtype t) { return t == XGEN_F32 ? (const void *)append_kernel<XGEN_F32> : (const void *)append_kernel<XGEN_F16_F32ACC>; }
+static const void *read_for(xgen_dtype t) { return t == XGEN_F32 ? (const void *)read_kernel<XGEN_F32> : (const void *)read_kernel<XGEN_F16_F32ACC>; }
+
+// ---- checks ----------------------------------------------------------------------------------------------------------------------
+static xgen_status check_batch(const xgen_attention_batch *b, bool pointers) {
+    if (!b) return XGEN_ERR_INVALID_ARG;
+    if (b->sequences < 0 || b->sequences == INT32_MAX || b->rows < 0 || b->rows > INT32_MAX || b->longest < 0 || b->table_stride < 0 || b->table_stride > INT32_MAX)
+        return XGEN_ERR_SHAPE;
+    if (!pointers || b->sequences == 0 || b->rows == 0) return XGEN_OK;
+    if (b->longest < 1 || b->table_stride < 1) return XGEN_ERR_SHAPE;
+    if (!b->row_start_dev || !b->length_dev || !b->page_table_dev ||
+        ((uintptr_t)b->row_start_dev | (uintptr_t)b->length_dev | (uintptr_t)b->page_table_dev) % 4)
+        return XGEN_ERR_INVALID_ARG;
+    return XGEN_OK;
+}
+static xgen_status check_cache(const xgen_attention_cache *c) {
+    if (!c || !c->k_codes_dev || !c->v_codes_dev || !c->k_scale_dev || !c->v_scale_dev) return XGEN_ERR_INVALID_ARG;
+    if (((uintptr_t)c->k_codes_dev | (uintptr_t)c->v_codes_dev) % 16 || ((uintptr_t)c->k_scale_dev | (uintptr_t)c->v_scale_dev) % 4) return XGEN_ERR_INVALID_ARG;
+    if (c->pages < 1 || c->pages > INT32_MAX) return XGEN_ERR_SHAPE;
+    return XGEN_OK;
+}
+static Batch batch_of(const xgen_attention_batch &b) {
+    return {b.row_start_dev, b.length_dev, b.page_table_dev, b.table_stride, b.sequences, (int)b.rows, b.longest};
+}
+static Cache cache_of(const xgen_attention_packed &h, const xgen_attention_cache &c) {
+    return {{static_cast<int8_t *>(c.k_codes_dev), static_cast<int8_t *>(c.v_codes_dev)}, {c.k_scale_dev, c.v_scale_dev}, c.pages, h.d.kv_heads, h.d.page_tokens};
+}
+static Rotation rotation_of(const xgen_attention_packed &h) { return {h.d_freq, h.d.rotary, h.d.interleaved}; }
+static size_t span_bytes(int64_t rows, int64_t stride, int64_t width, size_t eb) { return ((size_t)(rows - 1) * stride + width) * eb; }
+// Whether the bytes meet any of the cache's.
+static bool in_cache(const xgen_attention_packed &h, const xgen_attention_cache &c, const void *p, size_t n) {
+    const size_t scales = (size_t)c.pages * h.d.kv_heads * 4, codes = (size_t)c.pages * h.d.kv_heads * h.d.page_tokens * h.d.head_dim;
+    return overlap(p, n, c.k_codes_dev, codes) || overlap(p, n, c.v_codes_dev, codes) || overlap(p, n, c.k_scale_dev, scales) || overlap(p, n, c.v_scale_dev, scales);
+}
+static int64_t workspace_of(const xgen_attention_packed &h) {
+    const int64_t w = h.workers;
+    return w * 2 * kRows * h.d.head_dim * 4 + w * 2 * kRows * 16 + (w * 4 + 2) * 8;
+}
+
+}  // namespace attention
+
+using namespace attention;
+
+extern "C" {
+
+xgen_status xgen_attention_pack(const xgen_attention_desc *d, const double *freq, int device, xgen_attention_packed **out) {
+    if (!d || !out) return XGEN_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (d->q_heads < 1 || d->kv_heads < 1 || d->q_heads % d->kv_heads || d->window < 0 || !(d->softmax_scale >= 0.0f) || !(d->softmax_scale < INFINITY) ||
+        (d->rotary > 0) != (freq != nullptr))
+        return XGEN_ERR_INVALID_ARG;
+    if (d->dtype != XGEN_F32 && d->dtype != XGEN_F16_F32ACC) return XGEN_ERR_UNSUPPORTED;
+    const int D = d->head_dim, pt = d->page_tokens;
+    if ((D != 32 && D != 64 && D != 96 && D != 128 && D != 192 && D != 256) || (pt != 16 && pt != 32 && pt != 64 && pt != 128)) return XGEN_ERR_UNSUPPORTED;
+    if (d->rotary < 0 || d->rotary > D || d->rotary % 2 || d->window > kLongest) return XGEN_ERR_UNSUPPORTED;
+    if (d->q_heads > 65535) return XGEN_ERR_SHAPE;
+    for (int u = 0; u < d->rotary / 2; ++u)
+        if (!std::isfinite(freq[u])) return XGEN_ERR_INVALID_ARG;
+    xgen_attention_packed *h = new (std::nothrow) xgen_attention_packed();
+    if (!h) return XGEN_ERR_ALLOC;
+    h->d = *d;
+    h->d.interleaved = d->interleaved ? 1 : 0;
+    if (h->d.softmax_scale == 0.0f) h->d.softmax_scale = (float)(1.0 / std::sqrt((double)D));
+    h->device = device;
+    if (device < 0) {
+        *out = h;
+        return XGEN_OK;
+    }
+    xgen_status st = XGEN_OK;
+    OnDevice on(device);
+    if (!on.ok) st = XGEN_ERR_CUDA;
+    auto good = [&](cudaError_t e, xgen_status as) { if (st == XGEN_OK && e != cudaSuccess) st = as; };
+    const Kernels k = kernels_for(h->d);
+    int per_sm = 0;
+    if (st == XGEN_OK) {
+        good(cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, device), XGEN_ERR_CUDA);
+        good(cudaFuncSetAttribute(k.narrow, cudaFuncAttributeMaxDynamicSharedMemorySize, k.shared), XGEN_ERR_CUDA);
+        good(cudaFuncSetAttribute(append_for(d->dtype), cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 256 * 4), XGEN_ERR_CUDA);
+        good(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.narrow, kThreads, k.shared), XGEN_ERR_CUDA);
+        if (st == XGEN_OK && per_sm < 1) st = XGEN_ERR_CUDA;
+        h->workers = h->sms * per_sm;
+        good(cudaMalloc((void **)&h->d_status, 4), XGEN_ERR_ALLOC);
+        if (st == XGEN_OK) good(cudaMemset(h->d_status, 0, 4), XGEN_ERR_CUDA);
+    }
+    if (st == XGEN_OK && d->rotary) {
+        const int pairs = d->rotary / 2;
+        uint64_t turns[128];
+        for (int u = 0; u < pairs; ++u) {
+            const long double whole = (long double)freq[u] / 6.283185307179586476925286766559005768L;
+            const long double part = whole - floorl(whole);
+            turns[u] = (uint64_t)fminl(part * 18446744073709551616.0L, 18446744073709551615.0L);
+        }
+        good(cudaMalloc((void **)&h->d_freq, pairs * 8), XGEN_ERR_ALLOC);
+        if (st == XGEN_OK) good(cudaMemcpy(h->d_freq, turns, pairs * 8, cudaMemcpyHostToDevice), XGEN_ERR_CUDA);
+    }
+    if (st == XGEN_OK) good(cudaDeviceSynchronize(), XGEN_ERR_CUDA);
+    if (st != XGEN_OK) {
+        cudaGetLastError();
+        xgen_attention_free(h);
+        return st;
+    }
+    *out = h;
+    return XGEN_OK;
+}
+
+xgen_status xgen_attention_append(const xgen_attention_packed *h, const void *k, const void *v, int64_t stride, const xgen_attention_batch *b,
+                                  const xgen_attention_cache *c, void *stream) {
+    if (!h) return XGEN_ERR_INVALID_ARG;
+    xgen_status st = check_batch(b, true);
+    if (st == XGEN_OK) st = check_cache(c);
+    if (st != XGEN_OK) return st;
+    const int64_t width = (int64_t)h->d.kv_heads * h->d.head_dim;
+    if (stride < width || stride > (1ll << 31)) return XGEN_ERR_SHAPE;
+    if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
+    if (!k || !v) return XGEN_ERR_INVALID_ARG;
+    const size_t eb = element_bytes(h->d.dtype), bytes = span_bytes(b->rows, stride, width, eb);
+    if (((uintptr_t)k | (uintptr_t)v) % eb || in_cache(*h, *c, k, bytes) || in_cache(*h, *c, v, bytes)) return XGEN_ERR_INVALID_ARG;
+    if (h->device < 0) return XGEN_ERR_CUDA;
+    AppendParams P{};
+    P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
+    P.in[0] = k; P.in[1] = v; P.stride = stride; P.dim = h->d.head_dim; P.status = h->d_status;
+    for (int i = 0; i < 2; ++i) P.vec[i] = (uintptr_t)P.in[i] % 16 == 0 && stride * eb % 16 == 0;
+    // Pages that n new tokens of a sequence reach: at most (n - 1)/page_tokens + 2, and not more than n.
+    int64_t pages = b->rows / h->d.page_tokens + 2 * (int64_t)b->sequences;
+    if (pages > b->rows) pages = b->rows;
+    OnDevice on(h->device);
+    if (!on.ok) return XGEN_ERR_CUDA;
+    void *args[] = {&P};
+    P.room = h->d.page_tokens < b->longest ? h->d.page_tokens : b->longest;
+    return launch(append_for(h->d.dtype), dim3((unsigned)pages, h->d.kv_heads, 2), dim3(kAppendThreads), (size_t)P.room * h->d.head_dim * 4, stream, args);
+}
+
+xgen_status xgen_attention_read(const xgen_attention_packed *h, const xgen_attention_batch *b, const xgen_attention_cache *c, xgen_dtype out_dtype,
+                                void *k, void *v, int64_t stride, void *stream) {
+    if (!h) return XGEN_ERR_INVALID_ARG;
+    xgen_status st = check_batch(b, true);
+    if (st == XGEN_OK) st = check_cache(c);
+    if (st != XGEN_OK) return st;
+    if (out_dtype != XGEN_F32 && out_dtype != XGEN_F16_F32ACC) return XGEN_ERR_UNSUPPORTED;
+    const int64_t width = (int64_t)h->d.kv_heads * h->d.head_dim;
+    if (stride < width || stride > (1ll << 31)) return XGEN_ERR_SHAPE;
+    if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
+    if (!k || !v) return XGEN_ERR_INVALID_ARG;
+    const size_t eb = element_bytes(out_dtype), bytes = span_bytes(b->rows, stride, width, eb);
+    if (((uintptr_t)k | (uintptr_t)v) % eb || in_cache(*h, *c, k, bytes) || in_cache(*h, *c, v, bytes)) return XGEN_ERR_INVALID_ARG;
+    if (h->device < 0) return XGEN_ERR_CUDA;
+    ReadParams P{};
+    P.batch = batch_of(*b); P.cache = cache_of(*h, *c);
+    P.out[0] = k; P.out[1] = v; P.stride = stride; P.dim = h->d.head_dim; P.status = h->d_status;
+    for (int i = 0; i < 2; ++i) P.vec[i] = (uintptr_t)P.out[i] % 16 == 0 && stride * eb % 16 == 0;
+    const int64_t blocks = (b->rows * (width / 16) + kReadThreads - 1) / kReadThreads;
+    if (blocks > INT32_MAX) return XGEN_ERR_SHAPE;
+    OnDevice on(h->device);
+    if (!on.ok) return XGEN_ERR_CUDA;
+    void *args[] = {&P};
+    return launch(read_for(out_dtype), dim3((unsigned)blocks, 2), dim3(kReadThreads), 0, stream, args);
+}
+
+xgen_status xgen_attention_workspace(const xgen_attention_packed *h, const xgen_attention_batch *b, int64_t *bytes) {
+    if (!h || !bytes) return XGEN_ERR_INVALID_ARG;
+    const xgen_status st = check_batch(b, false);
+    if (st != XGEN_OK) return st;
+    if (h->device < 0) return XGEN_ERR_CUDA;
+    *bytes = workspace_of(*h);
+    return XGEN_OK;
+}
+
+xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, int64_t q_stride, const xgen_attention_batch *b, const xgen_attention_cache *c,
+                               void *y, int64_t y_stride, void *workspace, void *stream) {
+    if (!h) return XGEN_ERR_INVALID_ARG;
+    xgen_status st = check_batch(b, true);
+    if (st == XGEN_OK) st = check_cache(c);
+    if (st != XGEN_OK) return st;
+    const int64_t width = (int64_t)h->d.q_heads * h->d.head_dim;
+    const int group = h->d.q_heads / h->d.kv_heads;
+    if (q_stride < width || y_stride < width || q_stride > (1ll << 31) || y_stride > (1ll << 31) || b->rows * group > INT32_MAX - kRows) return XGEN_ERR_SHAPE;
+    if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
+    if (!q || !y || !workspace) return XGEN_ERR_INVALID_ARG;
+    const size_t eb = element_bytes(h->d.dtype), y_bytes = span_bytes(b->rows, y_stride, width, eb);
+    if (((uintptr_t)q | (uintptr_t)y) % eb || (uintptr_t)workspace % 16 || overlap(y, y_bytes, q, span_bytes(b->rows, q_stride, width, eb)) ||
+        in_cache(*h, *c, y, y_bytes))
+        return XGEN_ERR_INVALID_ARG;
+    if (h->device < 0) return XGEN_ERR_CUDA;
+    if (overlap(workspace, workspace_of(*h), y, y_bytes) || in_cache(*h, *c, workspace, workspace_of(*h))) return XGEN_ERR_INVALID_ARG;
+    const Kernels k = kernels_for(h->d);
+    RunParams P{};
+    P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
+    P.q = q; P.y = y; P.q_stride = q_stride; P.y_stride = y_stride;
+    P.group = group; P.window = h->d.window;
+    P.scale = (float)((double)h->d.softmax_scale * 1.4426950408889634);
+    P.workers = h->workers; P.status = h->d_status;
+    P.partial = static_cast<float *>(workspace);
+    P.stats = reinterpret_cast<float4 *>(P.partial + (int64_t)P.workers * 2 * kRows * h->d.head_dim);
+    P.cut = reinterpret_cast<int64_t *>(P.stats + (int64_t)P.workers * 2 * kRows);
+    OnDevice on(h->device);
+    if (!on.ok) return XGEN_ERR_CUDA;
+    void *args[] = {&P};
+    st = launch(k.narrow, dim3(P.workers), dim3(kThreads), k.shared, stream, args);
+    if (st == XGEN_OK && P.workers > 1) st = launch(k.combine, dim3(P.workers - 1), dim3(kCombineThreads), 0, stream, args);
+    return st;
+}
+
+xgen_status xgen_attention_last_status(const xgen_attention_packed *h, void *stream) {
+    if (!h) return XGEN_ERR_INVALID_ARG;
+    if (h->device < 0) return XGEN_ERR_CUDA;
+    return take_status(h->device, h->d_status, stream);
+}
+
+void xgen_attention_free(xgen_attention_packed *h) {
+    if (!h) return;
+    if (h->device >= 0) {
+        OnDevice on(h->device);
+        if (on.ok) {
+            cudaFree(h->d_freq); cudaFree(h->d_status);
+        }
+    }
+    delete h;
+}
+
+}  // extern "C"
