@@ -133,6 +133,7 @@ template <int DT, int RP, int ROWS> __global__ void __launch_bounds__(kThreads) 
     __shared__ float row_scale[ROWS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int rank = (int)(blockIdx.x % kCluster);
+    let_next();
     wait_before();
     const Tile tile = find_tile<ROWS>(P, (int)(blockIdx.x / kCluster));
     if (tile.count == 0) return;                         // (the whole cluster alike)

@@ -8,8 +8,10 @@
 //         equal pieces, one for each block that the GPU holds at once; where a cut falls inside a tile's tokens the pieces
 //         leave partial results, which `combine_kernel` joins in their order.  So any mixture of lengths fills the GPU evenly.
 //
-// A code is an integer of at most 127, exact in fp16: the matrix instructions take codes widened to fp16 (by byte permutes
-// and one subtraction), the page's scales are applied to scores and probabilities in fp32.
+// Scores are exact integer products: a query row is a factor times integers of 16 bits (fp32: 24), split into two (three) signed
+// bytes, and integer matrix instructions multiply each with the key codes as they lie in the cache.  Values meet probabilities
+// in fp16 (fp32: in two parts): a code is exact there, widened by byte permutes and one subtraction.  The page's scales are
+// applied to scores and probabilities in fp32.
 #include <cmath>
 #include <climits>
 #include <cstring>
@@ -22,7 +24,7 @@
 struct xgen_attention_packed {
     xgen_attention_desc d;
     int device, sms;
-    int workers;                // blocks of narrow_kernel that the device holds at once
+    int workers[2];             // blocks of narrow_kernel that the device holds at once, for one eight of rows and two
     uint64_t *d_freq;           // [rotary/2] turns per position, as 64-bit fractions
     int *d_status;
 };
@@ -40,7 +42,7 @@ struct Cache {
     int8_t *codes[2];           // keys, values
     float *scale[2];
     int64_t pages;
-    int heads, page_tokens;
+    int heads, page_tokens, page_shift;
 };
 struct Rotation {
     const uint64_t *freq;
@@ -57,7 +59,7 @@ __device__ __forceinline__ Span span_of(const Batch &B, int s) {
 }
 // The page of a token, or -1.
 __device__ __forceinline__ int64_t page_of(const Batch &B, const Cache &C, int s, int token) {
-    const int at = token / C.page_tokens;
+    const int at = token >> C.page_shift;
     if (at >= B.table_stride) return -1;
     const int p = B.table[(int64_t)s * B.table_stride + at];
     return p >= 0 && p < C.pages ? p : -1;
@@ -67,9 +69,9 @@ __device__ __forceinline__ int2 pair_of(const Rotation &R, int u) {
     if (u >= R.rotary / 2 || R.interleaved) return make_int2(2 * u, 2 * u + 1);
     return make_int2(u, u + R.rotary / 2);
 }
-__device__ __forceinline__ void turn(const Rotation &R, int u, int position, float &a, float &b) {
+__device__ __forceinline__ void turn(uint64_t freq, int position, float &a, float &b) {
     // position times the frequency in turns, modulo one turn: the upper half of a 64-bit product that wraps
-    const int32_t frac = (int32_t)((R.freq[u] * (uint64_t)position) >> 32);
+    const int32_t frac = (int32_t)((freq * (uint64_t)position) >> 32);
     float s, c;
     sincospif((float)frac * 4.6566128730773926e-10f, &s, &c);        // 2^-31: half turns
     const float x = a * c - b * s, y = a * s + b * c;
@@ -98,6 +100,7 @@ template <int DT> __global__ void __launch_bounds__(kAppendThreads) append_kerne
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int which = blockIdx.z, head = blockIdx.y, H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens;
     const bool keys = which == 0;
+    let_next();
     wait_before();
 
     // the page: number `want` of those that the batch's new tokens reach
@@ -169,7 +172,7 @@ template <int DT> __global__ void __launch_bounds__(kAppendThreads) append_kerne
             const int2 at = pair_of(P.rotation, u);
             float *const e = entries + token * D;
             float a = e[at.x], b = e[at.y];
-            turn(P.rotation, u, lo + token, a, b);
+            turn(P.rotation.freq[u], lo + token, a, b);
             e[at.x] = a;
             e[at.y] = b;
         }
@@ -245,6 +248,7 @@ template <int DT> __global__ void __launch_bounds__(kReadThreads) read_kernel(co
     using T = typename Elem<DT>::T;
     const int which = blockIdx.y, H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens;
     const int per_row = H * D / 16;
+    let_next();
     wait_before();
     const int64_t i = (int64_t)blockIdx.x * kReadThreads + threadIdx.x;
     const int64_t row = i / per_row;
@@ -286,11 +290,16 @@ template <int DT> __global__ void __launch_bounds__(kReadThreads) read_kernel(co
 }
 
 // ---- run: few rows against a long cache ------------------------------------------------------------------------------------------
-constexpr int kRows = 16;            // rows of a tile: query rows times the query heads of one key head
 constexpr int kTokens = 16;          // tokens that a warp takes at a time, in one page
 constexpr float kLift = 32768.0f;
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = kWarps * kTokens;
 
+// Where a worker's piece of the line begins: the tile (its rows, the units that it takes, which unit of the line is its first), and the
+// length of a piece.
+struct __align__(16) Cut {
+    int64_t first, piece;
+    int units, row, n, head, row0, unused[3];       // units = 0: the worker has no piece
+};
 struct RunParams {
     Batch batch;
     Cache cache;
@@ -300,10 +309,10 @@ struct RunParams {
     int64_t q_stride, y_stride;
     int group, window;
     float scale;                     // softmax scale times log2(e)
-    float *partial;                  // [workers][2][kRows][dim] sums
-    float4 *stats;                   // [workers][2][kRows]: maximum, total, unit of the sums
-    int64_t *cut;                    // [workers][4]: sequence, tile of it, first unit of that tile, its units; behind them the length of a piece
-    int workers;
+    float *partial;                  // [workers][2][rows of a tile][dim] sums
+    float4 *stats;                   // [workers][2][rows of a tile]: maximum, total, unit of the sums
+    struct Cut *cut;                 // [workers]
+    int workers, early;
     int *status;
 };
 
@@ -311,7 +320,7 @@ struct RunParams {
 struct Sequence {
     int row, n, length, from, tiles, units;
 };
-__device__ __forceinline__ Sequence sequence_of(const RunParams &P, int s) {
+template <int ROWS> __device__ __forceinline__ Sequence sequence_of(const RunParams &P, int s) {
     const Span sp = span_of(P.batch, s);
     Sequence q;
     q.row = sp.row; q.n = sp.n;
@@ -322,17 +331,21 @@ __device__ __forceinline__ Sequence sequence_of(const RunParams &P, int s) {
     if (end < q.length && q.n > 0) atomicExch(P.status, 1);
     const int first = q.length - q.n;                     // the first row's position (may be negative)
     q.from = P.window > 0 && first - P.window + 1 > 0 ? (first - P.window + 1) / kTokens * kTokens : 0;
-    q.tiles = (int)(((int64_t)q.n * P.group + kRows - 1) / kRows);
+    q.tiles = (int)(((int64_t)q.n * P.group + ROWS - 1) / ROWS);
     q.units = q.n > 0 ? max((end - q.from + kUnit - 1) / kUnit, 1) : 0;
     return q;
 }
 
+// a / b for a >= 0, b > 0: mostly small enough for the short division.
+__device__ __forceinline__ int64_t quotient(int64_t a, int b) {
+    return a < (1ll << 32) ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // A place on the line of units: unit `unit` of tile `tile` (of key head `head`) of sequence `s`.
 struct Place {
     Sequence q;
     int s, head, tile, unit;
 };
-__device__ __forceinline__ void next_place(const RunParams &P, Place &c) {
+template <int ROWS> __device__ __forceinline__ void next_place(const RunParams &P, Place &c) {
     if (++c.unit < c.q.units) return;
     c.unit = 0;
     if (++c.tile < c.q.tiles) return;
@@ -341,7 +354,7 @@ __device__ __forceinline__ void next_place(const RunParams &P, Place &c) {
     c.head = 0;
     do {
         if (++c.s >= P.batch.sequences) return;
-        c.q = sequence_of(P, c.s);
+        c.q = sequence_of<ROWS>(P, c.s);
     } while (c.q.n == 0);
 }
 
@@ -360,6 +373,11 @@ __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
 __device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 // Two of the four codes of `r` (its signs flipped: 0 .. 255) as fp16: 1024 + code as bits, less 1152.
 template <int SELECT> __device__ __forceinline__ uint32_t widen_codes(uint32_t flipped) {
     const uint32_t b = __byte_perm(flipped, 0x64646464u, SELECT);
@@ -371,28 +389,49 @@ __device__ __forceinline__ uint32_t pack_half(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-template <int DT, int D> struct Narrow {
-    static constexpr bool SPLIT = DT == XGEN_F32;          // operands of 22 bits as two of 11
-    static constexpr bool Q_IN_REGISTERS = !SPLIT && D <= 128;
+__device__ __forceinline__ uint32_t turn_matrix(uint32_t v) {        // an 8 x 8 matrix of 16-bit elements, transposed
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// D[16][8] += A[16][32] B[32][8] in signed bytes, 32-bit sums.  Lane 4g + t holds of A bytes 4t .. 4t + 3 of rows g (a[0]) and g + 8 (a[1]),
+// and bytes 16 + 4t .. of both; of B rows 4t .. 4t + 3 of column g, and 16 + 4t ..; of D as in mma16.
+__device__ __forceinline__ void mma_bytes(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// DT: type.  D: components of a head.  NT: eights of query rows in a tile.  Tokens are the rows of the score product and query rows its
+// columns, so a tile of up to eight rows (all that a decoding step has of most models) wastes no more than its empty columns.
+template <int DT, int D, int NT> struct Narrow {
+    static constexpr bool SPLIT = DT == XGEN_F32;          // probabilities of 22 bits as two of 11
+    static constexpr int TERMS = SPLIT ? 3 : 2;            // bytes of a query component
+    static constexpr int ROWS = 8 * NT;
+    static constexpr bool Q_IN_REGISTERS = TERMS * NT * D <= 512;
     static constexpr int ROW = D + 16;                     // bytes of a token's codes in shared memory: 8 tokens meet no bank twice
     static constexpr int STAGES = D <= 64 ? 4 : D <= 128 ? 3 : 2;
     static constexpr int STAGE = 2 * kTokens * ROW;        // keys, values
-    static constexpr int Q_ROW = D + 8;                    // fp16 elements of a query row
-    static constexpr int Q_BYTES = kRows * Q_ROW * 2 * (SPLIT ? 2 : 1);
+    static constexpr int Q_ROW = D + 16;                   // bytes of a query row's term
+    static constexpr int Q_BYTES = TERMS * ROWS * Q_ROW;
     static constexpr int RING = kWarps * STAGES * STAGE;
-    static constexpr int SHARED = RING + Q_BYTES + kRows * D * 4;
+    static constexpr int SUM_ROW = D + 4;
+    static constexpr int SUMS = ROWS * SUM_ROW;
+    static constexpr int COPIES = NT == 1 ? 2 : 1;         // of the sums, for as many warps at a time
+    static constexpr int SHARED = RING + Q_BYTES + COPIES * SUMS * 4;
+    static constexpr int BLOCKS = D <= 128 ? 3 : D * NT <= 256 ? 2 : 1;
 };
 
-template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 3 : 1) narrow_kernel(const RunParams P) {
+template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Narrow<DT, D, NT>::BLOCKS) narrow_kernel(const RunParams P) {
     using T = typename Elem<DT>::T;
-    using N = Narrow<DT, D>;
+    using N = Narrow<DT, D, NT>;
+    constexpr int ROWS = N::ROWS, TERMS = N::TERMS;
     extern __shared__ __align__(16) unsigned char shared[];
     unsigned char *const ring = shared;
-    __half *const qs = reinterpret_cast<__half *>(shared + N::RING);
-    float *const sums = reinterpret_cast<float *>(shared + N::RING + N::Q_BYTES);        // [kRows][D]
+    int8_t *const qs = reinterpret_cast<int8_t *>(shared + N::RING);                     // [TERMS][ROWS][Q_ROW]
+    float *const sums = reinterpret_cast<float *>(shared + N::RING + N::Q_BYTES);        // [COPIES][ROWS][SUM_ROW]
     __shared__ float stage_scale[kWarps][N::STAGES][2];
-    __shared__ float row_factor[kRows];
-    __shared__ float row_most[kWarps][kRows], row_total[kWarps][kRows], warp_unit[kWarps];
+    __shared__ float row_factor[ROWS];
+    __shared__ float row_most[kWarps][ROWS], row_total[kWarps][ROWS], warp_unit[kWarps];
     __shared__ int64_t scan[kWarps + 1], start_units;
     __shared__ int start_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -408,7 +447,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
         const int s0 = min(tid * each, P.batch.sequences), s1 = min(s0 + each, P.batch.sequences);
         int64_t own = 0;
         for (int s = s0; s < s1; ++s) {
-            const Sequence q = sequence_of(P, s);
+            const Sequence q = sequence_of<ROWS>(P, s);
             own += (int64_t)H * q.tiles * q.units;
         }
         int64_t upto = own;
@@ -426,13 +465,13 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
             if (w < warp) before += scan[w + 1];
             all += scan[w + 1];
         }
-        const int64_t piece = max((all + P.workers - 1) / P.workers, (int64_t)1);
+        const int64_t piece = max(quotient(all + P.workers - 1, P.workers), (int64_t)1);
         const int64_t from = piece * worker;
         todo = min(piece, all - from);
         if (todo > 0 && before <= from && from < before + own) {
             int64_t left = from - before;
             for (int s = s0; s < s1; ++s) {
-                const Sequence q = sequence_of(P, s);
+                const Sequence q = sequence_of<ROWS>(P, s);
                 const int64_t u = (int64_t)H * q.tiles * q.units;
                 if (left < u) { start_s = s; start_units = left; break; }
                 left -= u;
@@ -440,21 +479,26 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
         }
         __syncthreads();
         if (todo <= 0) {
-            if (tid == 0) P.cut[worker * 4 + 3] = 0;
+            if (tid == 0) P.cut[worker].units = 0;
             return;
         }
         ahead.s = start_s;
-        ahead.q = sequence_of(P, ahead.s);
-        const int64_t tile = start_units / ahead.q.units;
-        skipped = start_units % ahead.q.units;
+        ahead.q = sequence_of<ROWS>(P, ahead.s);
+        const int64_t tile = quotient(start_units, ahead.q.units);
+        skipped = start_units - tile * ahead.q.units;
         ahead.unit = (int)skipped;
-        ahead.head = (int)(tile / ahead.q.tiles);
-        ahead.tile = (int)(tile % ahead.q.tiles);
-        if (tid == 0 && worker == 0) P.cut[(int64_t)P.workers * 4] = piece;
+        ahead.head = (int)quotient(tile, ahead.q.tiles);
+        ahead.tile = (int)(tile - (int64_t)ahead.head * ahead.q.tiles);
         if (tid == 0) {
-            int64_t *const c = P.cut + worker * 4;
-            c[0] = ahead.s; c[1] = tile; c[2] = from - skipped; c[3] = ahead.q.units;
+            Cut c;
+            c.first = from - skipped; c.piece = piece;
+            c.units = ahead.q.units; c.row = ahead.q.row; c.n = ahead.q.n; c.head = ahead.head; c.row0 = ahead.tile * ROWS;
+            P.cut[worker] = c;
         }
+        // Short pieces: the joining blocks may come as soon as there is room, and find their instructions and arguments in time.
+        // (With long ones they, and the kernel behind them, would take room on some SMs from the next call's blocks: 64 sequences of up to
+        // 8192 tokens one call after the other 188 us, and 130 with the next launch let go at the end.)
+        if (piece <= P.early) let_next();
     }
 
     // ---- tokens on their way: each warp its own
@@ -463,35 +507,44 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
     int64_t left_ahead = todo;
     auto token_of = [&](const Place &c) { return c.q.from + c.unit * kUnit + warp * kTokens; };
     auto entry_of = [&](const Place &c) {                  // the page table's entry (asked for one unit before it is needed)
-        const int at = token_of(c) / P.cache.page_tokens;
+        const int at = token_of(c) >> P.cache.page_shift;
         return token_of(c) < c.q.length && at < P.batch.table_stride ? P.batch.table[(int64_t)c.s * P.batch.table_stride + at] : -2;
     };
     int entry = entry_of(ahead);
+    int first_seen, last_seen;                             // tokens that some row of the tile sees
+    auto set_seen = [&] {
+        const int before = ahead.q.length - ahead.q.n;     // the first row's position
+        last_seen = min(ahead.q.length - 1, before + (ahead.tile * ROWS + ROWS - 1) / G);
+        first_seen = P.window > 0 ? before + ahead.tile * ROWS / G - P.window + 1 : 0;
+    };
+    set_seen();
+    // this lane's 16-byte pieces of a tile: row (lane + 32 i) / (D/16), column the rest
+    const int8_t *const k_codes = P.cache.codes[0] + lane * 16, *const v_codes = P.cache.codes[1] + lane * 16;
     auto fetch = [&](int stage) {
         if (left_ahead > 0) {
             const int token = token_of(ahead);
-            // what the tile's last row sees ends at its own position, what its first row sees begins a window before
-            const int first = ahead.q.length - ahead.q.n + ahead.tile * kRows / G;
-            const int last = min(ahead.q.length - 1, ahead.q.length - ahead.q.n + (ahead.tile * kRows + kRows - 1) / G);
-            const bool seen = token <= last && (P.window == 0 || token + kTokens - 1 > first - P.window);
             there &= ~(1u << stage);
             if (entry >= 0 && entry < P.cache.pages) {
-                if (seen) {
+                if (token <= last_seen && token + kTokens > first_seen) {
                     const int64_t at = (int64_t)entry * H + ahead.head;
-                    const int64_t from = (at * P.cache.page_tokens + token % P.cache.page_tokens) * D;
+                    const int64_t from = ((at << P.cache.page_shift) + (token & (P.cache.page_tokens - 1))) * D;
                     const uint32_t to = my_ring + stage * N::STAGE;
 #pragma unroll
                     for (int i = 0; i < D / 32; ++i) {
-                        const int c = lane + 32 * i, row = c / (D / 16), col = c % (D / 16);
-                        copy_async16(to + row * N::ROW + col * 16, P.cache.codes[0] + from + c * 16);
-                        copy_async16(to + (kTokens + row) * N::ROW + col * 16, P.cache.codes[1] + from + c * 16);
+                        const int c = lane + 32 * i, place = c / (D / 16) * N::ROW + c % (D / 16) * 16;
+                        copy_async16(to + place, k_codes + from + i * 512);
+                        copy_async16(to + kTokens * N::ROW + place, v_codes + from + i * 512);
                     }
                     if (lane < 2) copy_async4(smem_at(&stage_scale[warp][stage][lane]), P.cache.scale[lane] + at);
                     there |= 1u << stage;
                 }
             } else if (entry != -2 && lane == 0) atomicExch(P.status, 1);
             if (--left_ahead > 0) {
-                next_place(P, ahead);
+                if (ahead.unit + 1 < ahead.q.units) ++ahead.unit;
+                else {
+                    next_place<ROWS>(P, ahead);
+                    set_seen();
+                }
                 entry = entry_of(ahead);
             }
         }
@@ -506,32 +559,42 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
     bool whole = skipped == 0;
     int slot = 0;                                          // of the partial results: 0 for the piece's first tile
     while (todo > 0) {
-        // ---- one tile of rows: queries, turned, with a power of two for each row that brings them near 2^14
-        const int row0 = now.tile * kRows, rows = min(kRows, now.q.n * G - row0);
+        // ---- one tile of rows: queries, turned, as a factor times integers
+        const int row0 = now.tile * ROWS, rows = min(ROWS, now.q.n * G - row0);
         const int first_position = now.q.length - now.q.n;
-        for (int r = warp; r < kRows; r += kWarps) {
-            float v[D / 32 + 1];
-            unsigned most = 0;
-            const int i = (row0 + r) / G;
-            constexpr int PAIRS = (D / 2 + 31) / 32;
+        constexpr int PAIRS = (D / 2 + 31) / 32, MINE = ROWS / kWarps;
+        float v[MINE][2 * PAIRS];
+#pragma unroll
+        for (int w = 0; w < MINE; ++w) {                   // (all loads first)
+            const int r = warp + w * kWarps, i = (row0 + r) / G;
             const T *const q = static_cast<const T *>(P.q) + (int64_t)(now.q.row + i) * P.q_stride + (int64_t)(now.head * G + (row0 + r) % G) * D;
 #pragma unroll
             for (int p = 0; p < PAIRS; ++p) {
                 const int u = lane + 32 * p;
-                float a = 0.0f, b = 0.0f;
-                if (r < rows && u < D / 2) {
-                    const int2 at = pair_of(P.rotation, u);
-                    a = widen(q[at.x]);
-                    b = widen(q[at.y]);
-                    if (u < P.rotation.rotary / 2 && first_position + i >= 0) turn(P.rotation, u, first_position + i, a, b);
-                }
-                v[2 * p] = a;
-                v[2 * p + 1] = b;
-                most = max(most, max(__float_as_uint(a) & 0x7FFFFFFFu, __float_as_uint(b) & 0x7FFFFFFFu));
+                const int2 at = pair_of(P.rotation, u);
+                const bool in = r < rows && u < D / 2;
+                v[w][2 * p] = in ? widen(q[at.x]) : 0.0f;
+                v[w][2 * p + 1] = in ? widen(q[at.y]) : 0.0f;
             }
+        }
+#pragma unroll
+        for (int w = 0; w < MINE; ++w) {
+            const int r = warp + w * kWarps, i = (row0 + r) / G;
+            unsigned most = 0;
+            if (r < rows && first_position + i >= 0) {
+#pragma unroll
+                for (int p = 0; p < PAIRS; ++p) {
+                    const int u = lane + 32 * p;
+                    if (u < P.rotation.rotary / 2) turn(P.rotation.freq[u], first_position + i, v[w][2 * p], v[w][2 * p + 1]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 2 * PAIRS; ++p) most = max(most, __float_as_uint(v[w][p]) & 0x7FFFFFFFu);
             most = __reduce_max_sync(~0u, most);
-            const int e = most && most < 0x7F800000u ? max(exponent(__uint_as_float(most)), -100) - 14 : 0;
-            const float by = pow2(-e);
+            // the largest component becomes 127 * 2^8 (2^16); a row below 2^-100 is taken as if it reached that
+            constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
+            const bool finite = most < 0x7F800000u;
+            const float top = fmaxf(__uint_as_float(most), 7.8886e-31f), by = finite ? LIMIT / top : 0.0f;
 #pragma unroll
             for (int p = 0; p < PAIRS; ++p) {
                 const int u = lane + 32 * p;
@@ -539,131 +602,146 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
                     const int2 at = pair_of(P.rotation, u);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float x = v[2 * p + j] * by;
-                        const __half hi = __float2half_rn(x);
-                        qs[r * N::Q_ROW + (j ? at.y : at.x)] = hi;
-                        if (N::SPLIT) qs[(kRows + r) * N::Q_ROW + (j ? at.y : at.x)] = __float2half_rn(x - __half2float(hi));
+                        int x = finite ? min(max(__float2int_rn(v[w][2 * p + j] * by), -(int)LIMIT), (int)LIMIT) : 0;
+#pragma unroll
+                        for (int m = 0; m < TERMS; ++m) {  // lowest byte first
+                            const int low = m == TERMS - 1 ? x : (int)(int8_t)x;
+                            qs[(m * ROWS + r) * N::Q_ROW + (j ? at.y : at.x)] = (int8_t)low;
+                            x = (x - low) >> 8;
+                        }
                     }
                 }
             }
-            if (lane == 0) row_factor[r] = pow2(e) * P.scale;
+            if (lane == 0) row_factor[r] = finite ? top / LIMIT * P.scale : NAN;
         }
         __syncthreads();
-        uint2 qf[N::Q_IN_REGISTERS ? D / 16 : 1][2];
+        constexpr int KEPT = N::Q_IN_REGISTERS ? D / 32 : 1;
+        uint32_t qf[TERMS][NT][KEPT][2];
+        auto query = [&](int m, int n, int c, int h) {
+            return *reinterpret_cast<const uint32_t *>(qs + (m * ROWS + n * 8 + g) * N::Q_ROW + c * 32 + 16 * h + 4 * t);
+        };
         if (N::Q_IN_REGISTERS) {
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c)
+            for (int m = 0; m < TERMS; ++m)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) qf[c][r] = *reinterpret_cast<const uint2 *>(qs + (g + 8 * r) * N::Q_ROW + c * 16 + 4 * t);
-        }
-        float factor[2];
-        int position[2];                                   // of this lane's rows g and g + 8; -1 where there is no row
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            factor[r] = row_factor[g + 8 * r];
-            position[r] = g + 8 * r < rows ? first_position + (row0 + g + 8 * r) / G : -1;
+                    for (int c = 0; c < KEPT; ++c) { qf[m][n][c][0] = query(m, n, c, 0); qf[m][n][c][1] = query(m, n, c, 1); }
         }
+        float factor[NT][2];
+        int position[NT][2];                               // of this lane's rows 8 n + 2t and the next; -1 where there is no row
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r = 8 * n + 2 * t + j;
+                factor[n][j] = row_factor[r];
+                position[n][j] = r < rows ? first_position + (row0 + r) / G : -1;
+            }
         const int least_position = first_position + row0 / G;
 
-        float o[D / 8][4];
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, unit = 0.0f;     // unit: the values' scale that o is in
+        // o[n][c]: components 16c + 2g of rows 8n + 2t and 8n + 2t + 1, then component 16c + 2g + 1 of both
+        float o[NT][D / 16][4];
+        float m[NT][2], l[NT][2], unit = 0.0f;             // unit: the values' scale that o is in
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.0f;
+        for (int n = 0; n < NT; ++n) {
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) o[n][c][0] = o[n][c][1] = o[n][c][2] = o[n][c][3] = 0.0f;
+        }
 
         // ---- its tokens, as far as the piece goes
         const int units = (int)min(todo, (int64_t)(now.q.units - now.unit));
         const bool last_part = now.unit + units == now.q.units;
-        for (int u = 0; u < units; ++u) {
+        int token = token_of(now);
+        for (int u = 0; u < units; ++u, token += kUnit) {
             fetch(stage == 0 ? N::STAGES - 1 : stage - 1);
             copy_async_wait<N::STAGES - 1>();
             __syncwarp();
             if (there >> stage & 1) {
-                const int token = token_of(now);
                 const uint32_t k_at = my_ring + stage * N::STAGE + a_lane, v_at = k_at + kTokens * N::ROW;
                 const float k_scale = stage_scale[warp][stage][0], v_scale = stage_scale[warp][stage][1];
-                float s[2][4] = {};
+                int dot[TERMS][NT][4] = {};
 #pragma unroll
-                for (int c = 0; c < D / 16; c += 2) {
-                    uint32_t r[4];
-                    load_matrices(r, k_at + c * 16);
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t a[4];
+                    load_matrices(a, k_at + c * 32);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t a[4], low[4];
-                        if (N::Q_IN_REGISTERS) {
-                            a[0] = qf[N::Q_IN_REGISTERS ? c + h : 0][0].x; a[1] = qf[N::Q_IN_REGISTERS ? c + h : 0][1].x;
-                            a[2] = qf[N::Q_IN_REGISTERS ? c + h : 0][0].y; a[3] = qf[N::Q_IN_REGISTERS ? c + h : 0][1].y;
-                        } else {
-                            const uint2 u0 = *reinterpret_cast<const uint2 *>(qs + g * N::Q_ROW + (c + h) * 16 + 4 * t);
-                            const uint2 u1 = *reinterpret_cast<const uint2 *>(qs + (g + 8) * N::Q_ROW + (c + h) * 16 + 4 * t);
-                            a[0] = u0.x; a[1] = u1.x; a[2] = u0.y; a[3] = u1.y;
-                        }
-                        if (N::SPLIT) {
-                            const uint2 u0 = *reinterpret_cast<const uint2 *>(qs + (kRows + g) * N::Q_ROW + (c + h) * 16 + 4 * t);
-                            const uint2 u1 = *reinterpret_cast<const uint2 *>(qs + (kRows + g + 8) * N::Q_ROW + (c + h) * 16 + 4 * t);
-                            low[0] = u0.x; low[1] = u1.x; low[2] = u0.y; low[3] = u1.y;
-                        }
+                    for (int k = 0; k < TERMS; ++k)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {      // 8 tokens at a time
-                            const uint32_t f = r[2 * h + e] ^ 0x80808080u, b0 = widen_codes<0x4140>(f), b1 = widen_codes<0x4342>(f);
-                            if (N::SPLIT) mma16(s[e], low, b0, b1);
-                            mma16(s[e], a, b0, b1);
+                        for (int n = 0; n < NT; ++n) {
+                            if (N::Q_IN_REGISTERS) mma_bytes(dot[k][n], a, qf[k][n][N::Q_IN_REGISTERS ? c : 0][0], qf[k][n][N::Q_IN_REGISTERS ? c : 0][1]);
+                            else mma_bytes(dot[k][n], a, query(k, n, c, 0), query(k, n, c, 1));
                         }
-                    }
                 }
-                // scores in powers of two, what a row does not see out of them, the running maximum
-                float most[2] = {-INFINITY, -INFINITY};
+                // scores in powers of two, what a row does not see out of them, the running maximum (rows: g and g + 8 of the tokens)
                 const bool all_seen = token + kTokens - 1 <= least_position && P.window == 0;       // (what the rows behind the last one see is no matter)
+                float s[NT][4], shrink[NT][2], most[NT][2];
+                bool changed = false;
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int r = i >> 1, j = token + 8 * e + 2 * t + (i & 1);
-                        float x = s[e][i] * (k_scale * factor[r]);
-                        if (!all_seen && (j > position[r] || (P.window > 0 && j <= position[r] - P.window))) x = -INFINITY;
-                        s[e][i] = x;
-                        most[r] = x > most[r] || isnan(x) ? x : most[r];
+                        const int j = token + g + 8 * (i >> 1), p = position[n][i & 1];
+                        float x = TERMS == 3 ? fmaf((float)dot[TERMS - 1][n][i], 65536.0f, (float)(dot[1][n][i] * 256 + dot[0][n][i]))
+                                             : (float)(dot[1][n][i] * 256 + dot[0][n][i]);
+                        x *= k_scale * factor[n][i & 1];
+                        if (!all_seen && (j > p || (P.window > 0 && j <= p - P.window))) x = -INFINITY;
+                        s[n][i] = x;
                     }
-                float alpha[2], base[2];
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
+                    for (int j = 0; j < 2; ++j) {
+                        float x = max_or_nan(s[n][j], s[n][2 + j]);
 #pragma unroll
-                    for (int d = 1; d < 4; d <<= 1) {
-                        const float x = __shfl_xor_sync(~0u, most[r], d);
-                        most[r] = x > most[r] || isnan(x) ? x : most[r];
+                        for (int d = 4; d < 32; d <<= 1) x = max_or_nan(x, __shfl_xor_sync(~0u, x, d));
+                        most[n][j] = x;
+                        x = max_or_nan(m[n][j], x);
+                        const float base = x == -INFINITY ? 0.0f : x;
+                        shrink[n][j] = exp2_approx(m[n][j] - base);
+                        m[n][j] = x;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) s[n][2 * i + j] = exp2_approx(s[n][2 * i + j] - base);
+                        l[n][j] = l[n][j] * shrink[n][j] + (s[n][j] + s[n][2 + j]);
                     }
-                    const float now_m = m[r] > most[r] ? m[r] : most[r];
-                    base[r] = now_m == -INFINITY ? 0.0f : now_m;
-                    alpha[r] = exp2_approx(m[r] - base[r]);
-                    m[r] = now_m;
                 }
                 // probabilities times 2^15 (fp16 then holds them down to 2^-29 of the largest), values relative to the largest scale
-                float by = kLift, shrink = 1.0f;
+                float by = kLift;
                 if (v_scale > unit && v_scale < INFINITY) {
-                    shrink = unit / v_scale;
+                    const float x = unit / v_scale;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) { shrink[n][0] *= x; shrink[n][1] *= x; }
                     unit = v_scale;
-                } else if (unit > 0.0f) by = v_scale < INFINITY ? kLift * (v_scale / unit) : 0.0f;
+                } else if (v_scale != unit && unit > 0.0f) by = v_scale < INFINITY ? kLift * (v_scale / unit) : 0.0f;
                 if (!(v_scale < INFINITY)) {               // the rows that see some of the page are lost, the others are not
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        if (!(most[r] == -INFINITY)) l[r] = NAN;
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (!(most[n][j] == -INFINITY)) l[n][j] = NAN;
                 }
-                uint32_t p[4], p_low[4];
+                uint32_t p[NT][2], p_low[NT][2];           // as the second operand: rows (tokens) 2t .. and 2t + 8 .., column (query row) g
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int n = 0; n < NT; ++n) {
+                    changed |= shrink[n][0] != 1.0f || shrink[n][1] != 1.0f;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float x0 = exp2_approx(s[e][2 * r] - base[r]), x1 = exp2_approx(s[e][2 * r + 1] - base[r]);
-                        l[r] = e == 0 ? l[r] * alpha[r] + (x0 + x1) : l[r] + (x0 + x1);
-                        p[2 * e + r] = pack_half(x0 * by, x1 * by);
+                    for (int i = 0; i < 2; ++i) {
+                        const float x0 = s[n][2 * i] * by, x1 = s[n][2 * i + 1] * by;
+                        const uint32_t high = pack_half(x0, x1);
+                        p[n][i] = turn_matrix(high);
                         if (N::SPLIT) {
-                            const __half2 h = *reinterpret_cast<const __half2 *>(&p[2 * e + r]);
-                            p_low[2 * e + r] = pack_half(x0 * by - __low2float(h), x1 * by - __high2float(h));
+                            const __half2 h = *reinterpret_cast<const __half2 *>(&high);
+                            p_low[n][i] = turn_matrix(pack_half(x0 - __low2float(h), x1 - __high2float(h)));
                         }
                     }
-                const float f0 = alpha[0] * shrink, f1 = alpha[1] * shrink;
-                if (__any_sync(~0u, f0 != 1.0f || f1 != 1.0f)) {
+                }
+                if (__any_sync(~0u, changed)) {
 #pragma unroll
-                    for (int j = 0; j < D / 8; ++j) { o[j][0] *= f0; o[j][1] *= f0; o[j][2] *= f1; o[j][3] *= f1; }
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c) {
+                            o[n][c][0] *= shrink[n][0]; o[n][c][1] *= shrink[n][1]; o[n][c][2] *= shrink[n][0]; o[n][c][3] *= shrink[n][1];
+                        }
                 }
 #pragma unroll
                 for (int c = 0; c < D / 16; c += 2) {
@@ -672,160 +750,204 @@ template <int DT, int D> __global__ void __launch_bounds__(kThreads, D <= 128 ? 
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t x0 = r[2 * h] ^ 0x80808080u, x1 = r[2 * h + 1] ^ 0x80808080u;
-                        const uint32_t even0 = widen_codes<0x4240>(x0), even1 = widen_codes<0x4240>(x1);
-                        const uint32_t odd0 = widen_codes<0x4341>(x0), odd1 = widen_codes<0x4341>(x1);
-                        if (N::SPLIT) {
-                            mma16(o[2 * (c + h)], p_low, even0, even1);
-                            mma16(o[2 * (c + h) + 1], p_low, odd0, odd1);
+                        const uint32_t a[4] = {widen_codes<0x4240>(x0), widen_codes<0x4341>(x0), widen_codes<0x4240>(x1), widen_codes<0x4341>(x1)};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            if (N::SPLIT) mma16(o[n][c + h], a, p_low[n][0], p_low[n][1]);
+                            mma16(o[n][c + h], a, p[n][0], p[n][1]);
                         }
-                        mma16(o[2 * (c + h)], p, even0, even1);
-                        mma16(o[2 * (c + h) + 1], p, odd0, odd1);
                     }
                 }
                 __syncwarp();                              // the stage is free again
             }
             stage = stage + 1 == N::STAGES ? 0 : stage + 1;
-            ++now.unit;
         }
         todo -= units;
-
         // ---- the warps' shares together
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            l[r] += __shfl_xor_sync(~0u, l[r], 1);
-            l[r] += __shfl_xor_sync(~0u, l[r], 2);
-            if (t == 0) { row_most[warp][g + 8 * r] = m[r]; row_total[warp][g + 8 * r] = l[r]; }
-        }
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(~0u, l[n][j], d);
+                if (g == 0) { row_most[warp][8 * n + 2 * t + j] = m[n][j]; row_total[warp][8 * n + 2 * t + j] = l[n][j]; }
+            }
         if (lane == 0) warp_unit[warp] = unit;
         __syncthreads();
-        float top[2], total[2], mine[2];
-        float top_unit = 0.0f;
+        float top[NT][2], total[NT][2], mine[NT][2], top_unit = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top_unit = warp_unit[w] > top_unit || isnan(warp_unit[w]) ? warp_unit[w] : top_unit;
+        for (int w = 0; w < kWarps; ++w) top_unit = fmaxf(top_unit, warp_unit[w]);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            top[r] = -INFINITY;
-            total[r] = 0.0f;
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float x = row_most[w][g + 8 * r];
-                top[r] = x > top[r] || isnan(x) ? x : top[r];
+            for (int j = 0; j < 2; ++j) {
+                const int r = 8 * n + 2 * t + j;
+                top[n][j] = row_most[0][r];
+#pragma unroll
+                for (int w = 1; w < kWarps; ++w) top[n][j] = max_or_nan(top[n][j], row_most[w][r]);
+                const float base = top[n][j] == -INFINITY ? 0.0f : top[n][j];
+                total[n][j] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) total[n][j] += row_total[w][r] * exp2_approx(row_most[w][r] - base);
+                mine[n][j] = unit == 0.0f ? 0.0f : exp2_approx(m[n][j] - base) * (unit / top_unit);
             }
-            const float base = top[r] == -INFINITY ? 0.0f : top[r];
+        for (int w = 0; w < kWarps / N::COPIES; ++w) {
+            if (warp / N::COPIES == w) {
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) total[r] += row_total[w][g + 8 * r] * exp2_approx(row_most[w][g + 8 * r] - base);
-            mine[r] = unit == 0.0f ? 0.0f : exp2_approx(m[r] - base) * (unit / top_unit);
-        }
-        for (int w = 0; w < kWarps; ++w) {
-            if (warp == w) {
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c)
+                    for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float4 *const at = reinterpret_cast<float4 *>(sums + (g + 8 * r) * D + c * 16 + 4 * t);
-                        float4 v = w == 0 ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : *at;
-                        v.x += mine[r] * o[2 * c][2 * r];
-                        v.y += mine[r] * o[2 * c + 1][2 * r];
-                        v.z += mine[r] * o[2 * c][2 * r + 1];
-                        v.w += mine[r] * o[2 * c + 1][2 * r + 1];
-                        *at = v;
-                    }
+                        for (int j = 0; j < 2; ++j) {
+                            float2 *const at = reinterpret_cast<float2 *>(sums + warp % N::COPIES * N::SUMS + (8 * n + 2 * t + j) * N::SUM_ROW + c * 16 + 2 * g);
+                            float2 v = w == 0 ? make_float2(0.0f, 0.0f) : *at;
+                            v.x += mine[n][j] * o[n][c][j];
+                            v.y += mine[n][j] * o[n][c][2 + j];
+                            *at = v;
+                        }
             }
             __syncthreads();
         }
+        auto sum_at = [&](int r, int d) { return N::COPIES == 1 ? sums[r * N::SUM_ROW + d] : sums[r * N::SUM_ROW + d] + sums[N::SUMS + r * N::SUM_ROW + d]; };
         const bool complete = whole && last_part;
         if (complete) {
-            if (warp == 0 && t == 0) {
+            if (warp == 0 && g == 0) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) row_total[0][g + 8 * r] = total[r] == 0.0f ? 0.0f : top_unit / (total[r] * kLift);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) row_total[0][8 * n + 2 * t + j] = total[n][j] == 0.0f ? 0.0f : top_unit / (total[n][j] * kLift);
             }
             __syncthreads();
             for (int i = tid; i < rows * D; i += kThreads) {
                 const int r = i / D, row = (row0 + r) / G, head = now.head * G + (row0 + r) % G;
                 const float by = row_total[0][r];
-                static_cast<T *>(P.y)[(int64_t)(now.q.row + row) * P.y_stride + (int64_t)head * D + i % D] = narrow<T>(by == 0.0f ? 0.0f : sums[i] * by);
+                static_cast<T *>(P.y)[(int64_t)(now.q.row + row) * P.y_stride + (int64_t)head * D + i % D] =
+                    narrow<T>(by == 0.0f ? 0.0f : sum_at(r, i % D) * by);
             }
         } else {
-            float *const to = P.partial + ((int64_t)worker * 2 + slot) * kRows * D;
-            for (int i = tid; i < rows * D; i += kThreads) to[i] = sums[i];
-            if (warp == 0 && t == 0) {
+            float *const to = P.partial + ((int64_t)worker * 2 + slot) * ROWS * D;
+            for (int i = tid; i < rows * D; i += kThreads) to[i] = sum_at(i / D, i % D);
+            if (warp == 0 && g == 0) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) P.stats[((int64_t)worker * 2 + slot) * kRows + g + 8 * r] = make_float4(top[r], total[r], top_unit, 0.0f);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        P.stats[((int64_t)worker * 2 + slot) * ROWS + 8 * n + 2 * t + j] = make_float4(top[n][j], total[n][j], top_unit, 0.0f);
             }
         }
         __syncthreads();
         if (todo > 0) {                                    // on to the next tile of rows
-            --now.unit;
-            next_place(P, now);
+            now.unit = now.q.units - 1;
+            next_place<ROWS>(P, now);
             whole = true;
             slot = 1;
         }
     }
+    let_next();
     copy_async_wait<0>();
 }
 
-// Joins the partial results of the tile that the cut before `worker` falls into, if that is the tile's first cut.
-constexpr int kCombineThreads = 128;
-template <int DT, int D> __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const RunParams P) {
+// Joins the partial results of the tile that the cut before `worker` falls into, if that is the tile's first cut: four groups of threads
+// take the parts in turn.
+constexpr int kCombineThreads = 512, kGroups = 4, kGroup = kCombineThreads / kGroups;
+template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const RunParams P) {
     using T = typename Elem<DT>::T;
+    __shared__ float4 row_stat[ROWS];                     // maximum, unit, factor of the sums
+    __shared__ float4 shares[kGroups - 1][kGroup];
     const int worker = blockIdx.x + 1, tid = threadIdx.x;
+    let_next();
     wait_before();
-    const int64_t *const cut = P.cut + (int64_t)worker * 4;
-    const int64_t units = cut[3];
-    if (units == 0) return;
-    const int64_t piece = P.cut[(int64_t)P.workers * 4];
-    const int64_t base = cut[2], from = piece * worker;
-    if (base == from || base < from - piece) return;       // the cut is between two tiles, or not the tile's first
-    const int s = (int)cut[0];
-    const Sequence q = sequence_of(P, s);
-    const int head = (int)(cut[1] / q.tiles), tile = (int)(cut[1] % q.tiles);
-    const int row0 = tile * kRows, rows = min(kRows, q.n * P.group - row0);
-    const int last = (int)((base + units - 1) / piece);
-    auto slot_of = [&](int w) { return (int64_t)w * 2 + (base <= piece * w ? 0 : 1); };
-    for (int i = tid; i < rows * (D / 4); i += kCombineThreads) {
-        const int r = i / (D / 4), at = i % (D / 4) * 4;
-        float top = -INFINITY, unit = 0.0f;
-        for (int w = worker - 1; w <= last; ++w) {
-            const float4 x = P.stats[slot_of(w) * kRows + r];
-            top = x.x > top || isnan(x.x) ? x.x : top;
-            unit = fmaxf(unit, x.z);
+    const Cut c = P.cut[worker];
+    const int64_t from = c.piece * worker;
+    if (c.units == 0 || c.first == from || c.first < from - c.piece) return;      // no piece; the cut is between two tiles, or not the tile's first
+    const int rows = min(ROWS, c.n * P.group - c.row0);
+    const int parts = (int)quotient(c.first + c.units - 1, (int)min(c.piece, (int64_t)INT_MAX)) - (worker - 1) + 1;
+    // the first part is its worker's last tile (or all it has), the others are their workers' first
+    const int64_t first_slot = (int64_t)(worker - 1) * 2 + (c.first <= from - c.piece ? 0 : 1), next_slot = (int64_t)worker * 2;
+    auto slot_of = [&](int part) { return part == 0 ? first_slot : next_slot + 2 * (part - 1); };
+    {
+        // statistics of a row: 512 / ROWS threads each, of one warp or two
+        constexpr int PER = ROWS == 8 ? 32 : 16;          // (half of the threads idle with ROWS = 8)
+        const int r = tid / PER, k = tid % PER;
+        if (r < ROWS) {
+            float top = -INFINITY, unit = 0.0f;
+            for (int part = k; part < parts; part += PER) {
+                const float4 x = P.stats[slot_of(part) * ROWS + r];
+                top = max_or_nan(top, x.x);
+                unit = fmaxf(unit, x.z);
+            }
+#pragma unroll
+            for (int d = 1; d < PER; d <<= 1) {
+                top = max_or_nan(top, __shfl_xor_sync(~0u, top, d));
+                unit = fmaxf(unit, __shfl_xor_sync(~0u, unit, d));
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+            float total = 0.0f;
+            for (int part = k; part < parts; part += PER) {
+                const float4 x = P.stats[slot_of(part) * ROWS + r];
+                total += exp2_approx(x.x - base) * x.y;
+            }
+#pragma unroll
+            for (int d = 1; d < PER; d <<= 1) total += __shfl_xor_sync(~0u, total, d);
+            if (k == 0) row_stat[r] = make_float4(base, unit, total == 0.0f ? 0.0f : unit / (total * kLift), 0.0f);
         }
-        const float base_m = top == -INFINITY ? 0.0f : top;
-        float total = 0.0f;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int w = worker - 1; w <= last; ++w) {
-            const float4 x = P.stats[slot_of(w) * kRows + r];
-            const float4 o = *reinterpret_cast<const float4 *>(P.partial + (slot_of(w) * kRows + r) * D + at);
-            const float e = exp2_approx(x.x - base_m), f = x.z == 0.0f ? 0.0f : e * (x.z / unit);
-            total += e * x.y;
-            v.x += f * o.x; v.y += f * o.y; v.z += f * o.z; v.w += f * o.w;
+    }
+    __syncthreads();
+    const int group = tid / kGroup, in_group = tid % kGroup;
+    for (int i0 = 0; i0 < rows * (D / 4); i0 += kGroup) {
+        const int i = i0 + in_group, r = i / (D / 4), at = i % (D / 4) * 4;
+        const bool in = r < rows;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f), stat = v;
+        if (in) {
+            stat = row_stat[r];
+#pragma unroll 4
+            for (int part = group; part < parts; part += kGroups) {
+                const int64_t slot = slot_of(part);
+                const float4 x = P.stats[slot * ROWS + r];
+                const float4 o = *reinterpret_cast<const float4 *>(P.partial + (slot * ROWS + r) * D + at);
+                const float f = x.z == 0.0f ? 0.0f : exp2_approx(x.x - stat.x) * (x.z / stat.y);
+                v.x += f * o.x; v.y += f * o.y; v.z += f * o.z; v.w += f * o.w;
+            }
         }
-        const float by = total == 0.0f ? 0.0f : unit / (total * kLift);
-        T *const to = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + r) / P.group) * P.y_stride + (int64_t)(head * P.group + (row0 + r) % P.group) * D + at;
-        const float4 y = by == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
-        to[0] = narrow<T>(y.x); to[1] = narrow<T>(y.y); to[2] = narrow<T>(y.z); to[3] = narrow<T>(y.w);
+        if (group) shares[group - 1][in_group] = v;
+        __syncthreads();
+        if (group == 0 && in) {
+#pragma unroll
+            for (int k = 0; k < kGroups - 1; ++k) {
+                const float4 x = shares[k][in_group];
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            T *const to = static_cast<T *>(P.y) + (int64_t)(c.row + (c.row0 + r) / P.group) * P.y_stride + (int64_t)(c.head * P.group + (c.row0 + r) % P.group) * D + at;
+            const float4 y = stat.z == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * stat.z, v.y * stat.z, v.z * stat.z, v.w * stat.z);
+            to[0] = narrow<T>(y.x); to[1] = narrow<T>(y.y); to[2] = narrow<T>(y.z); to[3] = narrow<T>(y.w);
+        }
+        __syncthreads();
     }
 }
 
 // ---- which instance --------------------------------------------------------------------------------------------------------------
 struct Kernels {
     const void *narrow, *combine;
-    int shared;
+    int shared, rows;
 };
-template <int DT, int D> static Kernels kernels_of() {
-    return {(const void *)narrow_kernel<DT, D>, (const void *)combine_kernel<DT, D>, Narrow<DT, D>::SHARED};
+template <int DT, int D> static Kernels kernels_of(int nt) {
+    if (nt == 1) return {(const void *)narrow_kernel<DT, D, 1>, (const void *)combine_kernel<DT, D, 8>, Narrow<DT, D, 1>::SHARED, 8};
+    return {(const void *)narrow_kernel<DT, D, 2>, (const void *)combine_kernel<DT, D, 16>, Narrow<DT, D, 2>::SHARED, 16};
 }
-template <int DT> static Kernels kernels_dt(int dim) {
+template <int DT> static Kernels kernels_dt(int dim, int nt) {
     switch (dim) {
-    case 32: return kernels_of<DT, 32>();
-    case 64: return kernels_of<DT, 64>();
-    case 96: return kernels_of<DT, 96>();
-    case 128: return kernels_of<DT, 128>();
-    case 192: return kernels_of<DT, 192>();
-    default: return kernels_of<DT, 256>();
+    case 32: return kernels_of<DT, 32>(nt);
+    case 64: return kernels_of<DT, 64>(nt);
+    case 96: return kernels_of<DT, 96>(nt);
+    case 128: return kernels_of<DT, 128>(nt);
+    case 192: return kernels_of<DT, 192>(nt);
+    default: return kernels_of<DT, 256>(nt);
     }
 }
-static Kernels kernels_for(const xgen_attention_desc &d) { return d.dtype == XGEN_F32 ? kernels_dt<XGEN_F32>(d.head_dim) : kernels_dt<XGEN_F16_F32ACC>(d.head_dim); }
+// nt: eights of rows in a tile.
+static Kernels kernels_for(const xgen_attention_desc &d, int nt) {
+    return d.dtype == XGEN_F32 ? kernels_dt<XGEN_F32>(d.head_dim, nt) : kernels_dt<XGEN_F16_F32ACC>(d.head_dim, nt);
+}
 static const void *append_for(xgen_dtype t) { return t == XGEN_F32 ? (const void *)append_kernel<XGEN_F32> : (const void *)append_kernel<XGEN_F16_F32ACC>; }
 static const void *read_for(xgen_dtype t) { return t == XGEN_F32 ? (const void *)read_kernel<XGEN_F32> : (const void *)read_kernel<XGEN_F16_F32ACC>; }
 
@@ -851,7 +973,7 @@ static Batch batch_of(const xgen_attention_batch &b) {
     return {b.row_start_dev, b.length_dev, b.page_table_dev, b.table_stride, b.sequences, (int)b.rows, b.longest};
 }
 static Cache cache_of(const xgen_attention_packed &h, const xgen_attention_cache &c) {
-    return {{static_cast<int8_t *>(c.k_codes_dev), static_cast<int8_t *>(c.v_codes_dev)}, {c.k_scale_dev, c.v_scale_dev}, c.pages, h.d.kv_heads, h.d.page_tokens};
+    return {{static_cast<int8_t *>(c.k_codes_dev), static_cast<int8_t *>(c.v_codes_dev)}, {c.k_scale_dev, c.v_scale_dev}, c.pages, h.d.kv_heads, h.d.page_tokens, __builtin_ctz(h.d.page_tokens)};
 }
 static Rotation rotation_of(const xgen_attention_packed &h) { return {h.d_freq, h.d.rotary, h.d.interleaved}; }
 static size_t span_bytes(int64_t rows, int64_t stride, int64_t width, size_t eb) { return ((size_t)(rows - 1) * stride + width) * eb; }
@@ -860,9 +982,14 @@ static bool in_cache(const xgen_attention_packed &h, const xgen_attention_cache 
     const size_t scales = (size_t)c.pages * h.d.kv_heads * 4, codes = (size_t)c.pages * h.d.kv_heads * h.d.page_tokens * h.d.head_dim;
     return overlap(p, n, c.k_codes_dev, codes) || overlap(p, n, c.v_codes_dev, codes) || overlap(p, n, c.k_scale_dev, scales) || overlap(p, n, c.v_scale_dev, scales);
 }
-static int64_t workspace_of(const xgen_attention_packed &h) {
-    const int64_t w = h.workers;
-    return w * 2 * kRows * h.d.head_dim * 4 + w * 2 * kRows * 16 + (w * 4 + 2) * 8;
+// Eights of rows in the tiles of a call: one where that holds all that any sequence has.
+static int eights_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
+    return (int64_t)b.longest * (h.d.q_heads / h.d.kv_heads) <= 8 ? 1 : 2;
+}
+static int64_t workspace_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
+    const int nt = eights_of(h, b);
+    const int64_t w = h.workers[nt - 1], rows = 8 * nt;
+    return w * 2 * rows * h.d.head_dim * 4 + w * 2 * rows * 16 + w * (int64_t)sizeof(Cut);
 }
 
 }  // namespace attention
@@ -898,15 +1025,17 @@ xgen_status xgen_attention_pack(const xgen_attention_desc *d, const double *freq
     OnDevice on(device);
     if (!on.ok) st = XGEN_ERR_CUDA;
     auto good = [&](cudaError_t e, xgen_status as) { if (st == XGEN_OK && e != cudaSuccess) st = as; };
-    const Kernels k = kernels_for(h->d);
-    int per_sm = 0;
     if (st == XGEN_OK) {
         good(cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, device), XGEN_ERR_CUDA);
-        good(cudaFuncSetAttribute(k.narrow, cudaFuncAttributeMaxDynamicSharedMemorySize, k.shared), XGEN_ERR_CUDA);
+        for (int nt = 1; nt <= 2; ++nt) {
+            const Kernels k = kernels_for(h->d, nt);
+            int per_sm = 0;
+            good(cudaFuncSetAttribute(k.narrow, cudaFuncAttributeMaxDynamicSharedMemorySize, k.shared), XGEN_ERR_CUDA);
+            good(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.narrow, kThreads, k.shared), XGEN_ERR_CUDA);
+            if (st == XGEN_OK && per_sm < 1) st = XGEN_ERR_CUDA;
+            h->workers[nt - 1] = h->sms * per_sm;
+        }
         good(cudaFuncSetAttribute(append_for(d->dtype), cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 256 * 4), XGEN_ERR_CUDA);
-        good(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.narrow, kThreads, k.shared), XGEN_ERR_CUDA);
-        if (st == XGEN_OK && per_sm < 1) st = XGEN_ERR_CUDA;
-        h->workers = h->sms * per_sm;
         good(cudaMalloc((void **)&h->d_status, 4), XGEN_ERR_ALLOC);
         if (st == XGEN_OK) good(cudaMemset(h->d_status, 0, 4), XGEN_ERR_CUDA);
     }
@@ -989,7 +1118,7 @@ xgen_status xgen_attention_workspace(const xgen_attention_packed *h, const xgen_
     const xgen_status st = check_batch(b, false);
     if (st != XGEN_OK) return st;
     if (h->device < 0) return XGEN_ERR_CUDA;
-    *bytes = workspace_of(*h);
+    *bytes = workspace_of(*h, *b);
     return XGEN_OK;
 }
 
@@ -1001,7 +1130,7 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     if (st != XGEN_OK) return st;
     const int64_t width = (int64_t)h->d.q_heads * h->d.head_dim;
     const int group = h->d.q_heads / h->d.kv_heads;
-    if (q_stride < width || y_stride < width || q_stride > (1ll << 31) || y_stride > (1ll << 31) || b->rows * group > INT32_MAX - kRows) return XGEN_ERR_SHAPE;
+    if (q_stride < width || y_stride < width || q_stride > (1ll << 31) || y_stride > (1ll << 31) || b->rows * group > INT32_MAX - 64) return XGEN_ERR_SHAPE;
     if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
     if (!q || !y || !workspace) return XGEN_ERR_INVALID_ARG;
     const size_t eb = element_bytes(h->d.dtype), y_bytes = span_bytes(b->rows, y_stride, width, eb);
@@ -1009,17 +1138,18 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
         in_cache(*h, *c, y, y_bytes))
         return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
-    if (overlap(workspace, workspace_of(*h), y, y_bytes) || in_cache(*h, *c, workspace, workspace_of(*h))) return XGEN_ERR_INVALID_ARG;
-    const Kernels k = kernels_for(h->d);
+    if (overlap(workspace, workspace_of(*h, *b), y, y_bytes) || in_cache(*h, *c, workspace, workspace_of(*h, *b))) return XGEN_ERR_INVALID_ARG;
+    const int nt = eights_of(*h, *b);
+    const Kernels k = kernels_for(h->d, nt);
     RunParams P{};
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
     P.q = q; P.y = y; P.q_stride = q_stride; P.y_stride = y_stride;
     P.group = group; P.window = h->d.window;
     P.scale = (float)((double)h->d.softmax_scale * 1.4426950408889634);
-    P.workers = h->workers; P.status = h->d_status;
+    P.workers = h->workers[nt - 1]; P.status = h->d_status; P.early = 16;
     P.partial = static_cast<float *>(workspace);
-    P.stats = reinterpret_cast<float4 *>(P.partial + (int64_t)P.workers * 2 * kRows * h->d.head_dim);
-    P.cut = reinterpret_cast<int64_t *>(P.stats + (int64_t)P.workers * 2 * kRows);
+    P.stats = reinterpret_cast<float4 *>(P.partial + (int64_t)P.workers * 2 * k.rows * h->d.head_dim);
+    P.cut = reinterpret_cast<Cut *>(P.stats + (int64_t)P.workers * 2 * k.rows);
     OnDevice on(h->device);
     if (!on.ok) return XGEN_ERR_CUDA;
     void *args[] = {&P};

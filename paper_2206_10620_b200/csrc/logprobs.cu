@@ -196,6 +196,7 @@ template <int DT, bool ENTROPY> __global__ void __launch_bounds__(kThreads, 4) l
     const int64_t row = blockIdx.x / (unsigned)cluster;
     if (tid == 0) n_found = n_queue = 0;
     arrive(cluster);                            // (every block has begun, its counter is set: waited for below)
+    let_next();
     wait_before();
     const T *const x = static_cast<const T *>(P.x) + row * P.stride;
     const int V = P.vocab, top = P.top;

@@ -66,9 +66,9 @@ inline size_t element_bytes(xgen_dtype t) { return t == XGEN_F32 ? 4 : 2; }
 
 #ifdef __CUDACC__
 
-__device__ __forceinline__ void wait_before() {
-    asm volatile("griddepcontrol.launch_dependents;\n griddepcontrol.wait;" ::: "memory");
-}
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// From here on (every block has to get there, or end) the next launch on the stream may take what room there is.
+__device__ __forceinline__ void let_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <int DT> struct Elem;
 template <> struct Elem<XGEN_F32> { using T = float; };
