@@ -1,8 +1,9 @@
 // libpatconv: a paged key/value cache of 8 bits and attention over it, for sm_100a, and their C ABI.
 //
-// append  one block per page that new tokens reach, head, and keys or values: the new entries go through shared memory in
-//         fp32 (turned there, if keys), their largest magnitude decides the page's scale, codes leave 16 bytes at a time.
-// read    codes times scales, 16 codes a thread.
+// append  one block per page that new tokens reach, some heads, and keys or values: a head's new entries stay in registers as fp32
+//         (turned there, if keys) until their largest magnitude has decided the page's scale.  A token's angle is that of the page's first token, worked
+//         out once for each of a thread's pairs, and that of its slot, from a table made with the handle.
+// read    codes times scales; blocks as for append, 16 bytes of the result a thread at a time.
 // run     `narrow_kernel`: few query rows (up to 16 with all query heads of a key head) against the whole cache of a sequence, bound
 //         by the cache's bytes.  The work of a call is a line of units (64 tokens of one key head, for one tile of rows), cut into
 //         equal pieces, one for each block that the GPU holds at once; where a cut falls inside a tile's tokens the pieces
@@ -25,7 +26,7 @@ struct xgen_attention_packed {
     xgen_attention_desc d;
     int device, sms;
     int workers[2];             // blocks of narrow_kernel that the device holds at once, for one eight of rows and two
-    uint64_t *d_freq;           // [rotary/2] turns per position, as 64-bit fractions
+    uint64_t *d_freq;           // [rotary/2] turns per position, as 64-bit fractions; behind them the cosines and sines of the slots of a page
     int *d_status;
 };
 
@@ -46,6 +47,7 @@ struct Cache {
 };
 struct Rotation {
     const uint64_t *freq;
+    const float2 *slots;        // [page_tokens][rotary/2]: cosine and sine of slot times frequency
     int rotary, interleaved;
 };
 
@@ -69,14 +71,74 @@ __device__ __forceinline__ int2 pair_of(const Rotation &R, int u) {
     if (u >= R.rotary / 2 || R.interleaved) return make_int2(2 * u, 2 * u + 1);
     return make_int2(u, u + R.rotary / 2);
 }
-__device__ __forceinline__ void turn(uint64_t freq, int position, float &a, float &b) {
-    // position times the frequency in turns, modulo one turn: the upper half of a 64-bit product that wraps
+// Cosine and sine of position times frequency.
+__device__ __forceinline__ float2 angle(uint64_t freq, int position) {
+    // in turns, modulo one turn: the upper half of a 64-bit product that wraps
     const int32_t frac = (int32_t)((freq * (uint64_t)position) >> 32);
-    float s, c;
-    sincospif((float)frac * 4.6566128730773926e-10f, &s, &c);        // 2^-31: half turns
-    const float x = a * c - b * s, y = a * s + b * c;
+    float2 r;
+    sincospif((float)frac * 4.6566128730773926e-10f, &r.y, &r.x);    // 2^-31: half turns
+    return r;
+}
+__device__ __forceinline__ void turn(float2 by, float &a, float &b) {
+    const float x = a * by.x - b * by.y, y = a * by.y + b * by.x;
     a = x;
     b = y;
+}
+
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Two of the four codes of `r` (its signs flipped: 0 .. 255) as fp16: 1024 + code as bits, less 1152.
+template <int SELECT> __device__ __forceinline__ uint32_t widen_codes(uint32_t flipped) {
+    const uint32_t b = __byte_perm(flipped, 0x64646464u, SELECT);
+    const __half2 h = __hsub2(*reinterpret_cast<const __half2 *>(&b), __half2half2(__ushort_as_half(0x6480)));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// Tokens of one page that a batch's rows are.
+struct PagePart {
+    int64_t page;                     // -1: not there
+    int row, n, slot, first;          // first of the rows, number of them, slot of the first; position of the page's first token
+};
+// Page number `want` of those that the batch's rows reach, sequence by sequence; false where there are fewer.  Every lane of the warp takes part.
+__device__ __forceinline__ bool find_page(const Batch &B, const Cache &C, int want, PagePart &part) {
+    const int lane = threadIdx.x & 31, PT = C.page_tokens;
+    int seq = -1, page_at = 0;
+    int64_t before = 0;
+    for (int i0 = 0; i0 < B.sequences; i0 += 32) {
+        const int i = i0 + lane;
+        int first = 0, count = 0;
+        if (i < B.sequences) {
+            const int n = span_of(B, i).n, length = length_of(B, i);
+            const int p0 = max(length - n, 0);
+            if (n > 0 && length > p0) { first = p0 >> C.page_shift; count = ((length - 1) >> C.page_shift) - first + 1; }
+        }
+        int upto = count;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int v = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += v;
+        }
+        const unsigned hit = __ballot_sync(~0u, want < before + upto);
+        if (hit) {
+            const int at = __ffs(hit) - 1;
+            seq = i0 + at;
+            page_at = __shfl_sync(~0u, first, at) + (int)(want - before) - (__shfl_sync(~0u, upto, at) - __shfl_sync(~0u, count, at));
+            break;
+        }
+        before += __shfl_sync(~0u, upto, 31);
+    }
+    if (seq < 0) return false;
+    const Span sp = span_of(B, seq);
+    const int length = length_of(B, seq);
+    const int lo = max(max(length - sp.n, 0), page_at * PT);
+    const int hi = (int)min((int64_t)length, (int64_t)(page_at + 1) * PT);
+    part.n = hi - lo; part.slot = lo - page_at * PT; part.first = page_at * PT;
+    part.row = sp.row + (lo - (length - sp.n));
+    part.page = page_of(B, C, seq, lo);
+    return true;
 }
 
 // ---- append ------------------------------------------------------------------------------------------------------------------
@@ -86,149 +148,186 @@ struct AppendParams {
     Rotation rotation;
     const void *in[2];
     int64_t stride;
-    int dim, room;              // room: tokens that the shared memory holds
+    int dim, room, heads;       // tokens that a block can hold, heads that it takes
     bool vec[2];
     int *status;
 };
 
-constexpr int kAppendThreads = 128;
+constexpr int kAppendMost = 512;      // threads of a block: as many as it takes for kItems items each
+constexpr int kItems = 4;             // items of 8 pairs (16 components of a token) that a thread holds: 64 x 128 entries are 128 threads' work
 
-template <int DT> __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendParams P) {
+// How a thread's items of a token lie: two pieces of 8 neighbours, next to each other or (a half's and the other half's) apart, or any way.
+enum Lay { PLAIN, HALVES, PAIRS, ANY };
+
+// Heads [head0, head1) of the page.  Item i of thread `tid` is pairs 8 s .. 8 s + 7 of token tid / per_token + i * (threads / per_token), s =
+// tid % per_token (the number of threads is a multiple of per_token).
+template <int DT, int LAY> __device__ __forceinline__ void append_heads(const AppendParams &P, const PagePart &part, int which, int head0, int head1) {
     using T = typename Elem<DT>::T;
-    extern __shared__ __align__(16) float entries[];     // [new tokens of the page][dim]
-    __shared__ unsigned most_bits[kAppendThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int which = blockIdx.z, head = blockIdx.y, H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens;
-    const bool keys = which == 0;
+    __shared__ unsigned most_bits[2][kAppendMost / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+    const int H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens, R = P.rotation.rotary, pairs = R / 2;
+    const int per_token = D / 16, s = tid % per_token, token0 = tid / per_token, step = threads / per_token;
+    const bool turned = LAY == ANY ? which == 0 && R > 0 : LAY != PLAIN;
+    const bool apart = LAY == PLAIN || (LAY == HALVES ? 16 * s < R : LAY == ANY && turned && !P.rotation.interleaved && 16 * s < R);
+    const int at0 = apart ? 8 * s : 16 * s, at1 = apart ? 8 * s + (LAY == PLAIN ? D / 2 : pairs) : 16 * s + 8;          // (not in ANY)
+    float2 base[8];                                       // of this thread's pairs at the page's first token
+    if (turned) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) base[j] = 8 * s + j < pairs ? angle(P.rotation.freq[8 * s + j], part.first) : make_float2(1.0f, 0.0f);
+    }
+    const T *const in = static_cast<const T *>(P.in[which]) + (int64_t)(part.row + token0) * P.stride;
+    constexpr int W = sizeof(T) / 2;                      // 16-byte pieces of 8 components
+    uint4 raw[kItems][2 * W];
+    const auto ask = [&](int head) {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const T *const from = in + (int64_t)(i * step) * P.stride + head * D;
+            const bool there = token0 + i * step < part.n;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                raw[i][w] = there ? __ldg(reinterpret_cast<const uint4 *>(from + at0) + w) : make_uint4(0, 0, 0, 0);
+                raw[i][W + w] = there ? __ldg(reinterpret_cast<const uint4 *>(from + at1) + w) : make_uint4(0, 0, 0, 0);
+            }
+        }
+    };
+#pragma unroll 1
+    for (int head = head0; head < head1; ++head) {
+        // ---- the new entries in fp32
+        float v[kItems][16];
+        if (LAY != ANY) ask(head);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const T *const from = in + (int64_t)(i * step) * P.stride + head * D;
+            const bool there = token0 + i * step < part.n;
+            if (LAY == ANY) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {             // (in `apart` order, or neighbours)
+                    const int2 at = apart ? pair_of(P.rotation, 8 * s + j) : make_int2(16 * s + 2 * j, 16 * s + 2 * j + 1);
+                    const float x = there ? widen(from[at.x]) : 0.0f, y = there ? widen(from[at.y]) : 0.0f;
+                    if (apart) { v[i][j] = x; v[i][8 + j] = y; }
+                    else { v[i][2 * j] = x; v[i][2 * j + 1] = y; }
+                }
+            }
+        }
+        float *const scale_at = P.cache.scale[which] + part.page * H + head;
+        const float was = part.slot ? *scale_at : 0.0f;
+        float largest = 0.0f;                             // magnitude; as bits, a NaN is above infinity
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            if (LAY != ANY) {
+#pragma unroll
+                for (int w = 0; w < 2 * W; ++w) {
+                    const uint32_t u[4] = {raw[i][w].x, raw[i][w].y, raw[i][w].z, raw[i][w].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (DT == XGEN_F32) v[i][4 * w + k] = __uint_as_float(u[k]);
+                        else {
+                            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[k]));
+                            v[i][(8 * w + 2 * k) & 15] = f.x;
+                            v[i][(8 * w + 2 * k + 1) & 15] = f.y;
+                        }
+                    }
+                }
+            }
+            if (turned && token0 + i * step < part.n) {
+                const float2 *const by_slot = P.rotation.slots + (part.slot + token0 + i * step) * pairs + 8 * s;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (8 * s + j < pairs) {
+                        const float2 o = __ldg(by_slot + j), b = base[j];
+                        const float2 by = make_float2(b.x * o.x - b.y * o.y, b.y * o.x + b.x * o.y);
+                        if (apart) turn(by, v[i][j], v[i][8 + j]);
+                        else turn(by, v[i][2 * j], v[i][2 * j + 1]);
+                    }
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) largest = max_or_nan(largest, fabsf(v[i][j]));
+        }
+        unsigned most = __reduce_max_sync(~0u, __float_as_uint(largest));
+        if (lane == 0) most_bits[head & 1][warp] = most;
+        __syncthreads();
+        for (int i = 0; i < threads / 32; ++i) most = max(most, most_bits[head & 1][i]);
+        const float amax = __uint_as_float(most);
+
+        // ---- the scale
+        float scale = was;
+        int halvings = 0;
+        if (most >= 0x7F800000u || isnan(was)) scale = NAN;
+        else if (!(was > 0.0f)) {
+            scale = most ? fmaxf(amax / 127.0f, 1.17549435e-38f) : 0.0f;
+            halvings = 100;                               // older entries are 0
+        } else
+            while (amax > 127.5f * scale) { scale *= 2.0f; ++halvings; }
+        if (tid == 0) *scale_at = scale;
+
+        // ---- codes
+        int8_t *const codes = P.cache.codes[which] + (part.page * H + head) * (int64_t)PT * D;
+        if (halvings > 0) {
+            const float by = pow2(-min(halvings, 100));
+            for (int c = tid; c < part.slot * per_token; c += threads) {
+                uint4 old = reinterpret_cast<const uint4 *>(codes)[c];
+                int8_t q[16];
+                memcpy(q, &old, 16);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) q[i] = (int8_t)__float2int_rn((float)q[i] * by);
+                memcpy(&old, q, 16);
+                reinterpret_cast<uint4 *>(codes)[c] = old;
+            }
+        }
+        const float by = scale > 0.0f ? 1.0f / scale : 0.0f;
+        if (amax * by > 127.4f) {                         // some entry may round beyond 127
+            const float most_code = 127.0f * scale;
+#pragma unroll
+            for (int i = 0; i < kItems; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[i][j] = fminf(fmaxf(v[i][j], -most_code), most_code);
+        }
+        int8_t *const to0 = codes + (int64_t)(part.slot + token0) * D;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            if (token0 + i * step >= part.n) break;
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t q[4];                            // 1.5 * 2^23 added leaves the nearest integer in the lowest bits
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[k] = __float_as_uint(fmaf(v[i][4 * j + k], by, 12582912.0f));
+                w[j] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+            }
+            if (isnan(scale)) w[0] = w[1] = w[2] = w[3] = 0;
+            int8_t *const to = to0 + i * step * D;
+            if (LAY != ANY && apart) {
+                *reinterpret_cast<uint2 *>(to + at0) = make_uint2(w[0], w[1]);
+                *reinterpret_cast<uint2 *>(to + at1) = make_uint2(w[2], w[3]);
+            } else if (LAY == ANY && apart) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int2 at = pair_of(P.rotation, 8 * s + j);
+                    to[at.x] = (int8_t)(w[j >> 2] >> (8 * (j & 3)));
+                    to[at.y] = (int8_t)(w[2 + (j >> 2)] >> (8 * (j & 3)));
+                }
+            } else *reinterpret_cast<uint4 *>(to + 16 * s) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+template <int DT> __global__ void __launch_bounds__(kAppendMost, 1) append_kernel(const AppendParams P) {
+    const int tid = threadIdx.x, which = blockIdx.z;
     let_next();
     wait_before();
 
-    // the page: number `want` of those that the batch's new tokens reach
-    int seq = -1, page_at = 0;
-    {
-        int64_t before = 0;
-        const int want = blockIdx.x;
-        for (int i0 = 0; i0 < P.batch.sequences; i0 += 32) {
-            const int i = i0 + lane;
-            int first = 0, count = 0;
-            if (i < P.batch.sequences) {
-                const int n = span_of(P.batch, i).n, length = length_of(P.batch, i);
-                const int p0 = max(length - n, 0);
-                if (n > 0 && length > p0) { first = p0 / PT; count = (length - 1) / PT - first + 1; }
-            }
-            int upto = count;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int v = __shfl_up_sync(~0u, upto, d);
-                if (lane >= d) upto += v;
-            }
-            const unsigned hit = __ballot_sync(~0u, want < before + upto);
-            if (hit) {
-                const int at = __ffs(hit) - 1;
-                seq = i0 + at;
-                page_at = __shfl_sync(~0u, first, at) + (int)(want - before) - (__shfl_sync(~0u, upto, at) - __shfl_sync(~0u, count, at));
-                break;
-            }
-            before += __shfl_sync(~0u, upto, 31);
-        }
-    }
-    if (seq < 0) return;
-    const Span sp = span_of(P.batch, seq);
-    const int length = length_of(P.batch, seq);
-    const int lo = max(max(length - sp.n, 0), page_at * PT);
-    const int hi = (int)min((int64_t)length, (int64_t)(page_at + 1) * PT);
-    const int n = hi - lo, slot = lo - page_at * PT;
-    const int64_t page = page_of(P.batch, P.cache, seq, lo);
-    if (page < 0 || n > P.room) {
+    PagePart part;
+    if (!find_page(P.batch, P.cache, blockIdx.x, part)) return;
+    if (part.page < 0 || part.n > P.room) {
         if (tid == 0) atomicExch(P.status, 1);
         return;
     }
-    const T *const in = static_cast<const T *>(P.in[which]) + (int64_t)(sp.row + (lo - (length - sp.n))) * P.stride + (int64_t)head * D;
-
-    // ---- the new entries, in fp32
-    const int pieces = n * (D / 8);
-    for (int c = tid; c < pieces; c += kAppendThreads) {
-        const int token = c / (D / 8), at = c % (D / 8) * 8;
-        const T *const from = in + (int64_t)token * P.stride + at;
-        T v[8];
-        if (P.vec[which]) {
-            uint4 raw[sizeof(T) / 2];
-#pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = __ldg(reinterpret_cast<const uint4 *>(from) + i);
-            memcpy(v, raw, sizeof v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = from[i];
-        }
-        float *const to = entries + token * D + at;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) to[i] = widen(v[i]);
-    }
-    __syncthreads();
-    if (keys && P.rotation.rotary) {
-        const int pairs = P.rotation.rotary / 2;
-        for (int c = tid; c < n * pairs; c += kAppendThreads) {
-            const int token = c / pairs, u = c % pairs;
-            const int2 at = pair_of(P.rotation, u);
-            float *const e = entries + token * D;
-            float a = e[at.x], b = e[at.y];
-            turn(P.rotation.freq[u], lo + token, a, b);
-            e[at.x] = a;
-            e[at.y] = b;
-        }
-        __syncthreads();
-    }
-    unsigned most = 0;                                    // the largest magnitude, as bits: a NaN is above infinity
-    for (int c = tid; c < n * D; c += kAppendThreads) most = max(most, __float_as_uint(entries[c]) & 0x7FFFFFFFu);
-    most = __reduce_max_sync(~0u, most);
-    if (lane == 0) most_bits[warp] = most;
-    float *const scale_at = P.cache.scale[which] + page * H + head;
-    const float was = slot ? *scale_at : 0.0f;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kAppendThreads / 32; ++i) most = max(most, most_bits[i]);
-    const float amax = __uint_as_float(most);
-
-    // ---- the scale
-    float scale = was;
-    int halvings = 0;
-    if (most >= 0x7F800000u || isnan(was)) scale = NAN;
-    else if (!(was > 0.0f)) {
-        scale = most ? fmaxf(amax / 127.0f, 1.17549435e-38f) : 0.0f;
-        halvings = 100;                                   // older entries are 0
-    } else
-        while (amax > 127.5f * scale) { scale *= 2.0f; ++halvings; }
-    if (tid == 0) *scale_at = scale;
-
-    // ---- codes
-    int8_t *const codes = P.cache.codes[which] + (page * H + head) * (int64_t)PT * D;
-    if (halvings > 0) {
-        const float by = pow2(-min(halvings, 100));
-        for (int c = tid; c < slot * (D / 16); c += kAppendThreads) {
-            uint4 raw = reinterpret_cast<const uint4 *>(codes)[c];
-            int8_t q[16];
-            memcpy(q, &raw, 16);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) q[i] = (int8_t)__float2int_rn((float)q[i] * by);
-            memcpy(&raw, q, 16);
-            reinterpret_cast<uint4 *>(codes)[c] = raw;
-        }
-    }
-    const float by = scale > 0.0f ? 1.0f / scale : 0.0f;   // (0 for a NaN too: the codes are 0 then)
-    for (int c = tid; c < n * (D / 16); c += kAppendThreads) {
-        const float *const e = entries + c * 16;
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            w[i] = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int q = by > 0.0f ? min(max(__float2int_rn(e[4 * i + j] * by), -127), 127) : 0;
-                w[i] |= (uint32_t)(q & 255) << (8 * j);
-            }
-        }
-        reinterpret_cast<uint4 *>(codes + (int64_t)slot * D)[c] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    const int head0 = blockIdx.y * P.heads, head1 = min(head0 + P.heads, P.cache.heads);
+    const int R = which == 0 ? P.rotation.rotary : 0;
+    if (!P.vec[which] || (R % 16 && !P.rotation.interleaved)) append_heads<DT, ANY>(P, part, which, head0, head1);
+    else if (R == 0) append_heads<DT, PLAIN>(P, part, which, head0, head1);
+    else if (P.rotation.interleaved) append_heads<DT, PAIRS>(P, part, which, head0, head1);
+    else append_heads<DT, HALVES>(P, part, which, head0, head1);
 }
 
 // ---- read --------------------------------------------------------------------------------------------------------------------
@@ -237,55 +336,83 @@ struct ReadParams {
     Cache cache;
     void *out[2];
     int64_t stride;
-    int dim;
+    int dim, heads;             // heads that a block takes
+    uint32_t token_of;          // 2^32 / (pieces of 16 bytes of a token's head), rounded up: for the token of a piece by one product
     bool vec[2];
     int *status;
 };
 
 constexpr int kReadThreads = 256;
 
-template <int DT> __global__ void __launch_bounds__(kReadThreads) read_kernel(const ReadParams P) {
+template <int DT> __global__ void __launch_bounds__(kReadThreads, 5) read_kernel(const ReadParams P) {
     using T = typename Elem<DT>::T;
-    const int which = blockIdx.y, H = P.cache.heads, D = P.dim, PT = P.cache.page_tokens;
-    const int per_row = H * D / 16;
+    constexpr int E = 16 / sizeof(T), MINE = 4;           // a thread's pieces: MINE at a time, the same of every head
+    const int tid = threadIdx.x, H = P.cache.heads, D = P.dim, per_token = D / E;
     let_next();
     wait_before();
-    const int64_t i = (int64_t)blockIdx.x * kReadThreads + threadIdx.x;
-    const int64_t row = i / per_row;
-    if (row >= P.batch.rows) return;
-    const int head = (int)(i % per_row) / (D / 16), at = (int)(i % per_row) % (D / 16) * 16;
-    int lo = 0, hi = P.batch.sequences;                   // the first sequence that ends behind the row
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (P.batch.row_start[mid + 1] > row) hi = mid; else lo = mid + 1;
-    }
-    if (lo >= P.batch.sequences) return;
-    const Span sp = span_of(P.batch, lo);
-    if (row < sp.row) return;
-    const int64_t position = (int64_t)length_of(P.batch, lo) - (sp.row + sp.n - row);
-    if (position < 0) return;
-    const int64_t page = page_of(P.batch, P.cache, lo, (int)position);
-    uint4 raw = make_uint4(0, 0, 0, 0);
-    float scale = 0.0f;
-    if (page < 0) atomicExch(P.status, 1);
-    else {
-        scale = P.cache.scale[which][page * H + head];
-        raw = *reinterpret_cast<const uint4 *>(P.cache.codes[which] + ((page * H + head) * (int64_t)PT + position % PT) * D + at);
-    }
-    int8_t q[16];
-    memcpy(q, &raw, 16);
-    T v[16];
+    PagePart part;
+    if (!find_page(P.batch, P.cache, blockIdx.x, part)) return;
+    if (part.page < 0 && tid == 0) atomicExch(P.status, 1);
+    const int head0 = blockIdx.y * P.heads, head1 = min(head0 + P.heads, H), pieces = part.n * per_token;
+    const int64_t page_codes = ((part.page * H << P.cache.page_shift) + part.slot) * D, next_head = (int64_t)D << P.cache.page_shift;
+#pragma unroll 1
+    for (int piece0 = tid; piece0 < pieces; piece0 += kReadThreads * MINE) {
+        int from[MINE];
+        int64_t to[MINE];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = narrow<T>((float)q[j] * scale);
-    T *const to = static_cast<T *>(P.out[which]) + row * P.stride + head * D + at;
-    if (P.vec[which]) {
-        uint4 w[sizeof(T)];
-        memcpy(w, v, sizeof v);
+        for (int i = 0; i < MINE; ++i) {
+            const int piece = piece0 + i * kReadThreads, token = (int)__umulhi((uint32_t)piece, P.token_of), at = piece * E;
+            from[i] = at;
+            to[i] = (int64_t)(part.row + token) * P.stride + (at - token * D);
+        }
+#pragma unroll 1
+        for (int both = 2 * head0; both < 2 * head1; ++both) {
+            const int w = both & 1, head = both >> 1;
+            const float scale = part.page < 0 ? 0.0f : P.cache.scale[w][part.page * H + head];
+            const int8_t *const codes = P.cache.codes[w] + page_codes + head * next_head;
+            T *const out = static_cast<T *>(P.out[w]) + head * D;
+            uint32_t raw[MINE][E / 4];
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(T); ++j) reinterpret_cast<uint4 *>(to)[j] = w[j];
-    } else {
+            for (int i = 0; i < MINE; ++i) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) to[j] = v[j];
+                for (int j = 0; j < E / 4; ++j) raw[i][j] = 0;
+                if (part.page >= 0 && piece0 + i * kReadThreads < pieces) {
+                    if (E == 8) {
+                        const uint2 u = *reinterpret_cast<const uint2 *>(codes + from[i]);
+                        raw[i][0] = u.x;
+                        raw[i][E / 4 - 1] = u.y;
+                    } else raw[i][0] = *reinterpret_cast<const uint32_t *>(codes + from[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                if (piece0 + i * kReadThreads >= pieces) break;
+                T v[E];
+#pragma unroll
+                for (int j = 0; j < E / 4; ++j) {
+                    const uint32_t u = raw[i][j] ^ 0x80808080u, h[2] = {widen_codes<0x4140>(u), widen_codes<0x4342>(u)};
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+                        if constexpr (DT == XGEN_F32) {
+                            v[4 * j + 2 * k] = f.x * scale;
+                            v[4 * j + 2 * k + 1] = f.y * scale;
+                        } else {
+                            const __half2 o = __floats2half2_rn(f.x * scale, f.y * scale);
+                            memcpy(&v[4 * j + 2 * k], &o, 4);
+                        }
+                    }
+                }
+                if (P.vec[w]) {
+                    uint4 o;
+                    memcpy(&o, v, 16);
+                    *reinterpret_cast<uint4 *>(out + to[i]) = o;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) out[to[i] + j] = v[j];
+                }
+            }
+        }
     }
 }
 
@@ -372,17 +499,6 @@ __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
 }
 __device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ float max_or_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-// Two of the four codes of `r` (its signs flipped: 0 .. 255) as fp16: 1024 + code as bits, less 1152.
-template <int SELECT> __device__ __forceinline__ uint32_t widen_codes(uint32_t flipped) {
-    const uint32_t b = __byte_perm(flipped, 0x64646464u, SELECT);
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2 *>(&b), __half2half2(__ushort_as_half(0x6480)));
-    return *reinterpret_cast<const uint32_t *>(&h);
 }
 __device__ __forceinline__ uint32_t pack_half(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
@@ -585,7 +701,7 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
 #pragma unroll
                 for (int p = 0; p < PAIRS; ++p) {
                     const int u = lane + 32 * p;
-                    if (u < P.rotation.rotary / 2) turn(P.rotation.freq[u], first_position + i, v[w][2 * p], v[w][2 * p + 1]);
+                    if (u < P.rotation.rotary / 2) turn(angle(P.rotation.freq[u], first_position + i), v[w][2 * p], v[w][2 * p + 1]);
                 }
             }
 #pragma unroll
@@ -975,12 +1091,24 @@ static Batch batch_of(const xgen_attention_batch &b) {
 static Cache cache_of(const xgen_attention_packed &h, const xgen_attention_cache &c) {
     return {{static_cast<int8_t *>(c.k_codes_dev), static_cast<int8_t *>(c.v_codes_dev)}, {c.k_scale_dev, c.v_scale_dev}, c.pages, h.d.kv_heads, h.d.page_tokens, __builtin_ctz(h.d.page_tokens)};
 }
-static Rotation rotation_of(const xgen_attention_packed &h) { return {h.d_freq, h.d.rotary, h.d.interleaved}; }
+static Rotation rotation_of(const xgen_attention_packed &h) { return {h.d_freq, reinterpret_cast<const float2 *>(h.d_freq + h.d.rotary / 2), h.d.rotary, h.d.interleaved}; }
 static size_t span_bytes(int64_t rows, int64_t stride, int64_t width, size_t eb) { return ((size_t)(rows - 1) * stride + width) * eb; }
 // Whether the bytes meet any of the cache's.
 static bool in_cache(const xgen_attention_packed &h, const xgen_attention_cache &c, const void *p, size_t n) {
     const size_t scales = (size_t)c.pages * h.d.kv_heads * 4, codes = (size_t)c.pages * h.d.kv_heads * h.d.page_tokens * h.d.head_dim;
     return overlap(p, n, c.k_codes_dev, codes) || overlap(p, n, c.v_codes_dev, codes) || overlap(p, n, c.k_scale_dev, scales) || overlap(p, n, c.v_scale_dev, scales);
+}
+// Pages that the batch's rows reach, at most: n tokens of a sequence reach (n - 1)/page_tokens + 2 of them, and not more than n.
+static int64_t pages_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
+    const int64_t pages = b.rows / h.d.page_tokens + 2 * (int64_t)b.sequences;
+    return pages < b.rows ? pages : b.rows;
+}
+// Heads of a block that takes a page's tokens: as many as leave eight blocks to an SM, so that what a block spends on finding its page counts
+// little where there is much to do.  `sides`: 2 where keys and values go to blocks of their own.
+static int heads_of_block(const xgen_attention_packed &h, int64_t pages, int sides) {
+    int heads = 1;
+    while (heads < h.d.kv_heads && pages * sides * ((h.d.kv_heads + heads) / (heads + 1)) >= 8 * (int64_t)h.sms) ++heads;
+    return heads;
 }
 // Eights of rows in the tiles of a call: one where that holds all that any sequence has.
 static int eights_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
@@ -1035,20 +1163,29 @@ xgen_status xgen_attention_pack(const xgen_attention_desc *d, const double *freq
             if (st == XGEN_OK && per_sm < 1) st = XGEN_ERR_CUDA;
             h->workers[nt - 1] = h->sms * per_sm;
         }
-        good(cudaFuncSetAttribute(append_for(d->dtype), cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 256 * 4), XGEN_ERR_CUDA);
         good(cudaMalloc((void **)&h->d_status, 4), XGEN_ERR_ALLOC);
         if (st == XGEN_OK) good(cudaMemset(h->d_status, 0, 4), XGEN_ERR_CUDA);
     }
     if (st == XGEN_OK && d->rotary) {
         const int pairs = d->rotary / 2;
-        uint64_t turns[128];
-        for (int u = 0; u < pairs; ++u) {
+        std::vector<uint64_t> table;
+        try {
+            table.resize((size_t)pairs * (1 + h->d.page_tokens));
+        } catch (const std::bad_alloc &) {
+            st = XGEN_ERR_ALLOC;
+        }
+        for (int u = 0; u < pairs && st == XGEN_OK; ++u) {
             const long double whole = (long double)freq[u] / 6.283185307179586476925286766559005768L;
             const long double part = whole - floorl(whole);
-            turns[u] = (uint64_t)fminl(part * 18446744073709551616.0L, 18446744073709551615.0L);
+            table[u] = (uint64_t)fminl(part * 18446744073709551616.0L, 18446744073709551615.0L);
+            for (int slot = 0; slot < h->d.page_tokens; ++slot) {
+                const long double turns = part * slot, at = (turns - floorl(turns)) * 6.283185307179586476925286766559005768L;
+                const float cs[2] = {(float)cosl(at), (float)sinl(at)};
+                std::memcpy(&table[pairs + (size_t)slot * pairs + u], cs, 8);
+            }
         }
-        good(cudaMalloc((void **)&h->d_freq, pairs * 8), XGEN_ERR_ALLOC);
-        if (st == XGEN_OK) good(cudaMemcpy(h->d_freq, turns, pairs * 8, cudaMemcpyHostToDevice), XGEN_ERR_CUDA);
+        if (st == XGEN_OK) good(cudaMalloc((void **)&h->d_freq, table.size() * 8), XGEN_ERR_ALLOC);
+        if (st == XGEN_OK) good(cudaMemcpy(h->d_freq, table.data(), table.size() * 8, cudaMemcpyHostToDevice), XGEN_ERR_CUDA);
     }
     if (st == XGEN_OK) good(cudaDeviceSynchronize(), XGEN_ERR_CUDA);
     if (st != XGEN_OK) {
@@ -1077,14 +1214,16 @@ xgen_status xgen_attention_append(const xgen_attention_packed *h, const void *k,
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
     P.in[0] = k; P.in[1] = v; P.stride = stride; P.dim = h->d.head_dim; P.status = h->d_status;
     for (int i = 0; i < 2; ++i) P.vec[i] = (uintptr_t)P.in[i] % 16 == 0 && stride * eb % 16 == 0;
-    // Pages that n new tokens of a sequence reach: at most (n - 1)/page_tokens + 2, and not more than n.
-    int64_t pages = b->rows / h->d.page_tokens + 2 * (int64_t)b->sequences;
-    if (pages > b->rows) pages = b->rows;
+    const int64_t pages = pages_of(*h, *b);
     OnDevice on(h->device);
     if (!on.ok) return XGEN_ERR_CUDA;
     void *args[] = {&P};
-    P.room = h->d.page_tokens < b->longest ? h->d.page_tokens : b->longest;
-    return launch(append_for(h->d.dtype), dim3((unsigned)pages, h->d.kv_heads, 2), dim3(kAppendThreads), (size_t)P.room * h->d.head_dim * 4, stream, args);
+    const int tokens = h->d.page_tokens < b->longest ? h->d.page_tokens : b->longest;
+    const int per_token = h->d.head_dim / 16, step = h->d.head_dim % 96 ? 32 : 96;        // threads: whole warps, and whole tokens
+    const int threads = (tokens * per_token + step * kItems - 1) / (step * kItems) * step;
+    P.room = threads * kItems / per_token;
+    P.heads = heads_of_block(*h, pages, 2);
+    return launch(append_for(h->d.dtype), dim3((unsigned)pages, (h->d.kv_heads + P.heads - 1) / P.heads, 2), dim3(threads), 0, stream, args);
 }
 
 xgen_status xgen_attention_read(const xgen_attention_packed *h, const xgen_attention_batch *b, const xgen_attention_cache *c, xgen_dtype out_dtype,
@@ -1104,13 +1243,15 @@ xgen_status xgen_attention_read(const xgen_attention_packed *h, const xgen_atten
     ReadParams P{};
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c);
     P.out[0] = k; P.out[1] = v; P.stride = stride; P.dim = h->d.head_dim; P.status = h->d_status;
+    const uint32_t per_token = (uint32_t)h->d.head_dim * (uint32_t)eb / 16;
+    P.token_of = (uint32_t)(((1ull << 32) + per_token - 1) / per_token);   // (exact below 2^26 pieces: per_token is at most 64, a page has at most 2^13)
     for (int i = 0; i < 2; ++i) P.vec[i] = (uintptr_t)P.out[i] % 16 == 0 && stride * eb % 16 == 0;
-    const int64_t blocks = (b->rows * (width / 16) + kReadThreads - 1) / kReadThreads;
-    if (blocks > INT32_MAX) return XGEN_ERR_SHAPE;
+    const int64_t pages = pages_of(*h, *b);
+    P.heads = heads_of_block(*h, pages, 1);
     OnDevice on(h->device);
     if (!on.ok) return XGEN_ERR_CUDA;
     void *args[] = {&P};
-    return launch(read_for(out_dtype), dim3((unsigned)blocks, 2), dim3(kReadThreads), 0, stream, args);
+    return launch(read_for(out_dtype), dim3((unsigned)pages, (h->d.kv_heads + P.heads - 1) / P.heads), dim3(kReadThreads), 0, stream, args);
 }
 
 xgen_status xgen_attention_workspace(const xgen_attention_packed *h, const xgen_attention_batch *b, int64_t *bytes) {
