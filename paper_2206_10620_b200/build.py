@@ -13,8 +13,8 @@ _INC = os.path.join(os.path.dirname(_HERE), "include")
 LIB_PATH = os.path.join(_HERE, "libpatconv.so")
 CALLS_PATH = os.path.join(_HERE, "_calls.abi3.so")     # the enqueueing calls for Python
 _SOURCES = ["patconv.cu", "tapgemm.cu", "tapgemm_f32.cu", "tapgemm_f16.cu", "tapgemm_f16_cut.cu", "tapgemm_i8.cu", "fewconv.cu", "blockgemm.cu", "dwconv.cu", "probe.cu", "pack.cpp",
-            "adapters.cu", "attention.cu", "logprobs.cu"]
-_DEPS = _SOURCES + ["patconv_internal.h", "ptx.cuh", "serve.cuh", "tapgemm.h", "tapgemm_kernel.cuh", "fewconv.h", "gen_core.py", "gen_blockgemm.py", os.path.join(_INC, "patconv.h"),
+            "adapters.cu", "attention.cu", "attention_wide.cu", "logprobs.cu"]
+_DEPS = _SOURCES + ["patconv_internal.h", "ptx.cuh", "serve.cuh", "attention.cuh", "tapgemm.h", "tapgemm_kernel.cuh", "fewconv.h", "gen_core.py", "gen_blockgemm.py", os.path.join(_INC, "patconv.h"),
                     os.path.join(_INC, "blockgemm.h"), os.path.join(_INC, "dwconv.h"), os.path.join(_INC, "adapters.h"),
                     os.path.join(_INC, "attention.h"), os.path.join(_INC, "logprobs.h")]
 
@@ -32,7 +32,9 @@ _INCLUDES = {
     "probe.cu": [os.path.join(_INC, "patconv.h")],
     "pack.cpp": ["patconv_internal.h", os.path.join(_INC, "patconv.h")],
     **{name + ".cu": ["patconv_internal.h", "serve.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, name + ".h")]
-       for name in ("adapters", "attention", "logprobs")},
+       for name in ("adapters", "logprobs")},
+    **{name + ".cu": ["patconv_internal.h", "ptx.cuh", "serve.cuh", "attention.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, "attention.h")]
+       for name in ("attention", "attention_wide")},
 }
 
 

@@ -427,7 +427,7 @@ xgen_status xgen_adapters_run(const xgen_adapters_packed *h, const void *x, int6
 xgen_status xgen_adapters_last_status(const xgen_adapters_packed *h, void *stream) {
     if (!h) return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
-    return take_status(h->device, h->d_status, stream);
+    return take_status(h->device, h->d_status, 1, stream);
 }
 
 void xgen_adapters_free(xgen_adapters_packed *h) {

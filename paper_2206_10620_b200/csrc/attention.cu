@@ -19,83 +19,18 @@
 #include <new>
 #include <vector>
 
-#include "attention.h"
-#include "serve.cuh"
+#include "attention.cuh"
 
 struct xgen_attention_packed {
     xgen_attention_desc d;
     int device, sms;
     int workers[2];             // blocks of narrow_kernel that the device holds at once, for one eight of rows and two
+    int wide_workers;           // blocks of wide_kernel, or 0 where there is none
     uint64_t *d_freq;           // [rotary/2] turns per position, as 64-bit fractions; behind them the cosines and sines of the slots of a page
     int *d_status;
 };
 
 namespace attention {
-using namespace serve;
-
-// The batch and the cache as the kernels see them.
-struct Batch {
-    const int32_t *row_start, *length, *table;
-    int64_t table_stride;
-    int sequences, rows, longest;
-};
-struct Cache {
-    int8_t *codes[2];           // keys, values
-    float *scale[2];
-    int64_t pages;
-    int heads, page_tokens, page_shift;
-};
-struct Rotation {
-    const uint64_t *freq;
-    const float2 *slots;        // [page_tokens][rotary/2]: cosine and sine of slot times frequency
-    int rotary, interleaved;
-};
-
-constexpr int kLongest = 1 << 30;    // tokens of a sequence
-__device__ __forceinline__ int length_of(const Batch &B, int s) { return min(max(B.length[s], 0), kLongest); }
-// First row and number of rows of a sequence.
-struct Span { int row, n; };
-__device__ __forceinline__ Span span_of(const Batch &B, int s) {
-    const int lo = min(max(B.row_start[s], 0), B.rows);
-    return {lo, max(min(B.row_start[s + 1], B.rows) - lo, 0)};
-}
-// The page of a token, or -1.
-__device__ __forceinline__ int64_t page_of(const Batch &B, const Cache &C, int s, int token) {
-    const int at = token >> C.page_shift;
-    if (at >= B.table_stride) return -1;
-    const int p = B.table[(int64_t)s * B.table_stride + at];
-    return p >= 0 && p < C.pages ? p : -1;
-}
-// Components of pair u of a head of `dim`: those behind the turned ones pair up too, for convenience.
-__device__ __forceinline__ int2 pair_of(const Rotation &R, int u) {
-    if (u >= R.rotary / 2 || R.interleaved) return make_int2(2 * u, 2 * u + 1);
-    return make_int2(u, u + R.rotary / 2);
-}
-// Cosine and sine of position times frequency.
-__device__ __forceinline__ float2 angle(uint64_t freq, int position) {
-    // in turns, modulo one turn: the upper half of a 64-bit product that wraps
-    const int32_t frac = (int32_t)((freq * (uint64_t)position) >> 32);
-    float2 r;
-    sincospif((float)frac * 4.6566128730773926e-10f, &r.y, &r.x);    // 2^-31: half turns
-    return r;
-}
-__device__ __forceinline__ void turn(float2 by, float &a, float &b) {
-    const float x = a * by.x - b * by.y, y = a * by.y + b * by.x;
-    a = x;
-    b = y;
-}
-
-__device__ __forceinline__ float max_or_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-// Two of the four codes of `r` (its signs flipped: 0 .. 255) as fp16: 1024 + code as bits, less 1152.
-template <int SELECT> __device__ __forceinline__ uint32_t widen_codes(uint32_t flipped) {
-    const uint32_t b = __byte_perm(flipped, 0x64646464u, SELECT);
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2 *>(&b), __half2half2(__ushort_as_half(0x6480)));
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
 
 // Tokens of one page that a batch's rows are.
 struct PagePart {
@@ -418,30 +353,8 @@ template <int DT> __global__ void __launch_bounds__(kReadThreads, 5) read_kernel
 
 // ---- run: few rows against a long cache ------------------------------------------------------------------------------------------
 constexpr int kTokens = 16;          // tokens that a warp takes at a time, in one page
-constexpr float kLift = 32768.0f;
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = kWarps * kTokens;
 
-// Where a worker's piece of the line begins: the tile (its rows, the units that it takes, which unit of the line is its first), and the
-// length of a piece.
-struct __align__(16) Cut {
-    int64_t first, piece;
-    int units, row, n, head, row0, unused[3];       // units = 0: the worker has no piece
-};
-struct RunParams {
-    Batch batch;
-    Cache cache;
-    Rotation rotation;
-    const void *q;
-    void *y;
-    int64_t q_stride, y_stride;
-    int group, window;
-    float scale;                     // softmax scale times log2(e)
-    float *partial;                  // [workers][2][rows of a tile][dim] sums
-    float4 *stats;                   // [workers][2][rows of a tile]: maximum, total, unit of the sums
-    struct Cut *cut;                 // [workers]
-    int workers, early;
-    int *status;
-};
 
 // What a sequence asks for: rows, tiles of rows for each key head, units of a tile, where its tokens begin.
 struct Sequence {
@@ -458,15 +371,12 @@ template <int ROWS> __device__ __forceinline__ Sequence sequence_of(const RunPar
     if (end < q.length && q.n > 0) atomicExch(P.status, 1);
     const int first = q.length - q.n;                     // the first row's position (may be negative)
     q.from = P.window > 0 && first - P.window + 1 > 0 ? (first - P.window + 1) / kTokens * kTokens : 0;
+    if (P.launched > 1 && q.n * P.group > kNarrowMost) q.n = 0;        // another kernel's
     q.tiles = (int)(((int64_t)q.n * P.group + ROWS - 1) / ROWS);
     q.units = q.n > 0 ? max((end - q.from + kUnit - 1) / kUnit, 1) : 0;
     return q;
 }
 
-// a / b for a >= 0, b > 0: mostly small enough for the short division.
-__device__ __forceinline__ int64_t quotient(int64_t a, int b) {
-    return a < (1ll << 32) ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
 // A place on the line of units: unit `unit` of tile `tile` (of key head `head`) of sequence `s`.
 struct Place {
     Sequence q;
@@ -485,38 +395,11 @@ template <int ROWS> __device__ __forceinline__ void next_place(const RunParams &
     } while (c.q.n == 0);
 }
 
-__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy_async16(uint32_t to, const void *from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_async4(uint32_t to, const void *from) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ uint32_t pack_half(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
 __device__ __forceinline__ uint32_t turn_matrix(uint32_t v) {        // an 8 x 8 matrix of 16-bit elements, transposed
     uint32_t r;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// D[16][8] += A[16][32] B[32][8] in signed bytes, 32-bit sums.  Lane 4g + t holds of A bytes 4t .. 4t + 3 of rows g (a[0]) and g + 8 (a[1]),
-// and bytes 16 + 4t .. of both; of B rows 4t .. 4t + 3 of column g, and 16 + 4t ..; of D as in mma16.
-__device__ __forceinline__ void mma_bytes(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
 // DT: type.  D: components of a head.  NT: eights of query rows in a tile.  Tokens are the rows of the score product and query rows its
 // columns, so a tile of up to eight rows (all that a decoding step has of most models) wastes no more than its empty columns.
 template <int DT, int D, int NT> struct Narrow {
@@ -982,8 +865,8 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
     const int64_t first_slot = (int64_t)(worker - 1) * 2 + (c.first <= from - c.piece ? 0 : 1), next_slot = (int64_t)worker * 2;
     auto slot_of = [&](int part) { return part == 0 ? first_slot : next_slot + 2 * (part - 1); };
     {
-        // statistics of a row: 512 / ROWS threads each, of one warp or two
-        constexpr int PER = ROWS == 8 ? 32 : 16;          // (half of the threads idle with ROWS = 8)
+        // statistics of a row: some threads of one warp
+        constexpr int PER = kCombineThreads / ROWS > 32 ? 32 : kCombineThreads / ROWS;
         const int r = tid / PER, k = tid % PER;
         if (r < ROWS) {
             float top = -INFINITY, unit = 0.0f;
@@ -1005,7 +888,7 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
             }
 #pragma unroll
             for (int d = 1; d < PER; d <<= 1) total += __shfl_xor_sync(~0u, total, d);
-            if (k == 0) row_stat[r] = make_float4(base, unit, total == 0.0f ? 0.0f : unit / (total * kLift), 0.0f);
+            if (k == 0) row_stat[r] = make_float4(base, unit, total == 0.0f ? 0.0f : unit / (total * P.lift), 0.0f);
         }
     }
     __syncthreads();
@@ -1043,12 +926,12 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
 
 // ---- which instance --------------------------------------------------------------------------------------------------------------
 struct Kernels {
-    const void *narrow, *combine;
+    const void *narrow, *combine, *combine_wide;
     int shared, rows;
 };
 template <int DT, int D> static Kernels kernels_of(int nt) {
-    if (nt == 1) return {(const void *)narrow_kernel<DT, D, 1>, (const void *)combine_kernel<DT, D, 8>, Narrow<DT, D, 1>::SHARED, 8};
-    return {(const void *)narrow_kernel<DT, D, 2>, (const void *)combine_kernel<DT, D, 16>, Narrow<DT, D, 2>::SHARED, 16};
+    if (nt == 1) return {(const void *)narrow_kernel<DT, D, 1>, (const void *)combine_kernel<DT, D, 8>, (const void *)combine_kernel<DT, D, kWideRows>, Narrow<DT, D, 1>::SHARED, 8};
+    return {(const void *)narrow_kernel<DT, D, 2>, (const void *)combine_kernel<DT, D, 16>, (const void *)combine_kernel<DT, D, kWideRows>, Narrow<DT, D, 2>::SHARED, 16};
 }
 template <int DT> static Kernels kernels_dt(int dim, int nt) {
     switch (dim) {
@@ -1110,14 +993,28 @@ static int heads_of_block(const xgen_attention_packed &h, int64_t pages, int sid
     while (heads < h.d.kv_heads && pages * sides * ((h.d.kv_heads + heads) / (heads + 1)) >= 8 * (int64_t)h.sms) ++heads;
     return heads;
 }
-// Eights of rows in the tiles of a call: one where that holds all that any sequence has.
-static int eights_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
-    return (int64_t)b.longest * (h.d.q_heads / h.d.kv_heads) <= 8 ? 1 : 2;
+// Which kernels a call launches.
+struct Route {
+    int eights;                 // narrow_kernel's tiles, in eights of rows; 0: not launched
+    bool wide;
+};
+// Up to 16 rows of every sequence (with all query heads of a key head) are narrow_kernel's, in tiles of eight where that holds them.  Where there
+// may be more, wide_kernel takes the sequences that have more, and narrow_kernel is launched too unless all must have.
+// us at 16 and 32 rows of 8 sequences over 8192 tokens: see the comment at kNarrowMost's use in DESIGN's table of cases.
+static Route route_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
+    const int64_t group = h.d.q_heads / h.d.kv_heads, most = (int64_t)b.longest * group;
+    if (most <= 8) return {1, false};
+    if (most <= kNarrowMost || !h.wide_workers || b.sequences > kWideSequences) return {2, false};
+    const int64_t least = b.rows - (int64_t)(b.sequences - 1) * b.longest;       // rows of the shortest sequence, at least
+    return {least * group > kNarrowMost ? 0 : 2, true};
 }
+static int64_t part_bytes(const xgen_attention_packed &h, int64_t workers, int64_t rows) {
+    return (workers * 2 * rows * (h.d.head_dim * 4 + 16) + workers * (int64_t)sizeof(Cut) + 255) / 256 * 256;
+}
+static int64_t narrow_bytes(const xgen_attention_packed &h, const Route &r) { return r.eights ? part_bytes(h, h.workers[r.eights - 1], 8 * r.eights) : 0; }
 static int64_t workspace_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
-    const int nt = eights_of(h, b);
-    const int64_t w = h.workers[nt - 1], rows = 8 * nt;
-    return w * 2 * rows * h.d.head_dim * 4 + w * 2 * rows * 16 + w * (int64_t)sizeof(Cut);
+    const Route r = route_of(h, b);
+    return narrow_bytes(h, r) + (r.wide ? part_bytes(h, h.wide_workers, kWideRows) : 0);
 }
 
 }  // namespace attention
@@ -1163,8 +1060,13 @@ xgen_status xgen_attention_pack(const xgen_attention_desc *d, const double *freq
             if (st == XGEN_OK && per_sm < 1) st = XGEN_ERR_CUDA;
             h->workers[nt - 1] = h->sms * per_sm;
         }
-        good(cudaMalloc((void **)&h->d_status, 4), XGEN_ERR_ALLOC);
-        if (st == XGEN_OK) good(cudaMemset(h->d_status, 0, 4), XGEN_ERR_CUDA);
+        const WideKernel wide = wide_kernel_for(h->d.dtype, h->d.head_dim);
+        if (wide.kernel) {
+            good(cudaFuncSetAttribute(wide.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, wide.shared), XGEN_ERR_CUDA);
+            h->wide_workers = h->sms * wide.blocks;
+        }
+        good(cudaMalloc((void **)&h->d_status, 8), XGEN_ERR_ALLOC);
+        if (st == XGEN_OK) good(cudaMemset(h->d_status, 0, 8), XGEN_ERR_CUDA);
     }
     if (st == XGEN_OK && d->rotary) {
         const int pairs = d->rotary / 2;
@@ -1280,29 +1182,42 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
         return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
     if (overlap(workspace, workspace_of(*h, *b), y, y_bytes) || in_cache(*h, *c, workspace, workspace_of(*h, *b))) return XGEN_ERR_INVALID_ARG;
-    const int nt = eights_of(*h, *b);
-    const Kernels k = kernels_for(h->d, nt);
+    const Route route = route_of(*h, *b);
     RunParams P{};
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
     P.q = q; P.y = y; P.q_stride = q_stride; P.y_stride = y_stride;
     P.group = group; P.window = h->d.window;
     P.scale = (float)((double)h->d.softmax_scale * 1.4426950408889634);
-    P.workers = h->workers[nt - 1]; P.status = h->d_status; P.early = 16;
-    P.partial = static_cast<float *>(workspace);
-    P.stats = reinterpret_cast<float4 *>(P.partial + (int64_t)P.workers * 2 * k.rows * h->d.head_dim);
-    P.cut = reinterpret_cast<Cut *>(P.stats + (int64_t)P.workers * 2 * k.rows);
+    P.status = h->d_status; P.early = 16;
+    P.launched = (route.eights ? 1 : 0) + (route.wide ? 1 : 0);
     OnDevice on(h->device);
     if (!on.ok) return XGEN_ERR_CUDA;
-    void *args[] = {&P};
-    st = launch(k.narrow, dim3(P.workers), dim3(kThreads), k.shared, stream, args);
-    if (st == XGEN_OK && P.workers > 1) st = launch(k.combine, dim3(P.workers - 1), dim3(kCombineThreads), 0, stream, args);
+    // a kernel over tiles of `rows` rows, and the joining of what its workers leave in pieces
+    const auto attend = [&](const void *kernel, const void *combine, int workers, int rows, int threads, int shared, char *work) {
+        P.workers = workers;
+        P.lift = rows == kWideRows ? kWideLift : kLift;
+        P.partial = reinterpret_cast<float *>(work);
+        P.stats = reinterpret_cast<float4 *>(P.partial + (int64_t)workers * 2 * rows * h->d.head_dim);
+        P.cut = reinterpret_cast<Cut *>(P.stats + (int64_t)workers * 2 * rows);
+        void *args[] = {&P};
+        xgen_status r = launch(kernel, dim3(workers), dim3(threads), shared, stream, args);
+        if (r == XGEN_OK && workers > 1) r = launch(combine, dim3(workers - 1), dim3(kCombineThreads), 0, stream, args);
+        return r;
+    };
+    const Kernels k = kernels_for(h->d, route.eights ? route.eights : 1);
+    char *const work = static_cast<char *>(workspace);
+    if (route.eights) st = attend(k.narrow, k.combine, h->workers[route.eights - 1], k.rows, kThreads, k.shared, work);
+    if (st == XGEN_OK && route.wide) {
+        const WideKernel w = wide_kernel_for(h->d.dtype, h->d.head_dim);
+        st = attend(w.kernel, k.combine_wide, h->wide_workers, kWideRows, kWideThreads, w.shared, work + narrow_bytes(*h, route));
+    }
     return st;
 }
 
 xgen_status xgen_attention_last_status(const xgen_attention_packed *h, void *stream) {
     if (!h) return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
-    return take_status(h->device, h->d_status, stream);
+    return take_status(h->device, h->d_status, 2, stream);
 }
 
 void xgen_attention_free(xgen_attention_packed *h) {

@@ -1,0 +1,529 @@
+// libpatconv: attention of many query rows over the paged cache of 8 bits, on the 5th-generation tensor cores (sm_100a).
+//
+// A block takes 128 rows (query rows times the query heads of one key head), one to a thread, and goes through their tokens 64 at
+// a time.  Tensor memory holds the scores [128][64] and the sums [128][dim]:
+//   * scores: kind::i8, the queries' bytes (two, fp32 three, see attention.cu) against the key codes as they lie in the cache, one
+//     accumulator per byte; a thread reads its row's 64 integers and has its softmax without any exchange;
+//   * probabilities go to shared memory as fp16 (fp32: in two parts), value codes are widened to fp16 there, rows of tokens being the
+//     contiguous direction (the operand is given as transposed), and kind::f16 adds their product to the sums.
+// The sums are rescaled only where a row's maximum rises by more than 2^7 (or the values' scale doubles): probabilities are
+// lifted by 2^7, so that fp16 holds what that leaves.
+// The order of a step keeps the tensor cores fed: while the product of step j and the scores of step j + 1 run, back to back, the
+// threads widen the values of step j + 1; codes of step j + 2 are on their way.  Two blocks to an SM fill each other's gaps.
+//
+// The work is cut into equal pieces as in attention.cu; units are counted tile by tile here, since a causal tile of an early row takes
+// few of them.
+//
+// Bound by the matrix units and the exponentials about alike (a unit of dim 128: 128 x 64 x 128 twice at 8192 multiply-adds a clock,
+// scores in two integer products at twice that, 256 clocks in all; 8192 exponentials at 16 a clock, 512 clocks).
+#include "attention.cuh"
+#include "ptx.cuh"
+
+namespace attention {
+using patconv::fence_async_proxy;
+using patconv::mbar_init;
+using patconv::mbar_wait;
+using patconv::mma_f16;
+using patconv::mma_i8;
+using patconv::operand_desc;
+using patconv::tc_commit;
+using patconv::tc_fence_after;
+using patconv::tc_fence_before;
+using patconv::tmem_alloc;
+using patconv::tmem_free;
+using patconv::tmem_ld16;
+using patconv::tmem_st16;
+using patconv::tmem_wait_ld;
+using patconv::tmem_wait_st;
+
+constexpr int kW = 4;                                     // warps
+constexpr float kFar = 7.0f;                              // (2^7 * 2^7 * 2, for values up to twice the unit, is within fp16)
+
+template <int DT, int D> struct Wide {
+    static constexpr bool SPLIT = DT == XGEN_F32;
+    static constexpr int TERMS = SPLIT ? 3 : 2;
+    static constexpr int CODES = kWideUnit * D;           // of keys, or values
+    static constexpr int Q = TERMS * kWideRows * D;
+    static constexpr int VALUES = kWideUnit * D * 2;
+    static constexpr int PROBS = kWideRows * kWideUnit * 2;
+    static constexpr int SHARED = Q + 4 * CODES + VALUES + PROBS * (SPLIT ? 2 : 1);
+    static constexpr int COLUMNS = TERMS * kWideUnit + D <= 256 ? 256 : 512;
+    static constexpr int BLOCKS = COLUMNS == 256 && SHARED <= 104 * 1024 ? 2 : 1;
+};
+
+// What a sequence asks for, and a tile of its rows.
+struct WideSequence { int row, n, length, end, tiles; };
+struct WideTile { int from, to, units; };                 // tokens [from, to) that some row sees
+__device__ __forceinline__ WideSequence wide_sequence(const RunParams &P, int s) {
+    const Span sp = span_of(P.batch, s);
+    WideSequence q;
+    q.row = sp.row; q.n = sp.n;
+    q.length = length_of(P.batch, s);
+    q.end = (int)min((int64_t)q.length, P.batch.table_stride * P.cache.page_tokens);
+    if (P.launched > 1 && q.n * P.group <= kNarrowMost) q.n = 0;
+    if (q.end < q.length && q.n > 0) atomicExch(P.status, 1);
+    q.tiles = (int)(((int64_t)q.n * P.group + kWideRows - 1) / kWideRows);
+    return q;
+}
+__device__ __forceinline__ WideTile wide_tile(const RunParams &P, const WideSequence &q, int tile) {
+    const int before = q.length - q.n, row0 = tile * kWideRows, row1 = min(q.n * P.group, row0 + kWideRows) - 1;
+    WideTile t;
+    t.from = P.window > 0 ? max(before + row0 / P.group - P.window + 1, 0) & ~15 : 0;
+    t.to = max(min(before + row1 / P.group + 1, q.end), t.from);
+    t.units = max((t.to - t.from + kWideUnit - 1) / kWideUnit, 1);
+    return t;
+}
+
+template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT, D>::BLOCKS) wide_kernel(const RunParams P) {
+    using T = typename Elem<DT>::T;
+    using W = Wide<DT, D>;
+    constexpr int TERMS = W::TERMS, CHUNKS = D / 16;
+    extern __shared__ __align__(128) unsigned char shared[];
+    int8_t *const qs = reinterpret_cast<int8_t *>(shared);                  // [TERMS][128 rows][D], 8 rows of 16 bytes contiguous
+    unsigned char *const codes = shared + W::Q;                             // [2 stages][keys, values][64 tokens][D], likewise
+    unsigned char *const values = codes + 4 * W::CODES;                     // fp16 [8 tokens of 16 bytes][D/8][8]
+    unsigned char *const probs = values + W::VALUES;                        // fp16 [128 rows][64 tokens], 8 rows of 16 bytes contiguous
+    __shared__ float stage_scale[2][2][4];
+    __shared__ int units_of[kWideSequences];
+    __shared__ int64_t scan[kW + 1], start_units;
+    __shared__ int start_s, start_tile, start_unit;
+    __shared__ float row_factor[kWideRows];
+    __shared__ __align__(8) uint64_t bars[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int H = P.cache.heads, G = P.group, worker = blockIdx.x;
+    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]);
+    wait_before();
+
+    // ---- this block's piece of the line of units: sequences, key heads, tiles, units
+    int64_t todo, skipped = 0, first_unit;
+    WideSequence q;
+    int s, head, tile;
+    {
+        const int S = P.batch.sequences;
+        for (int i = warp; i < S; i += kW) {
+            const WideSequence w = wide_sequence(P, i);
+            int u = 0;
+            for (int t = lane; t < w.tiles; t += 32) u += wide_tile(P, w, t).units;
+            u = (int)__reduce_add_sync(~0u, (unsigned)u);
+            if (lane == 0) units_of[i] = u;
+        }
+        if (tid == 0) {
+            scan[0] = 0;
+            s_abort = 0;
+            mbar_init(bar_s, 1);
+            mbar_init(bar_o, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncthreads();
+        const int each = (S + kWideThreads - 1) / kWideThreads, s0 = min(tid * each, S), s1 = min(s0 + each, S);
+        int64_t own = 0;
+        for (int i = s0; i < s1; ++i) own += (int64_t)H * units_of[i];
+        int64_t upto = own;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t v = __shfl_up_sync(~0u, upto, d);
+            if (lane >= d) upto += v;
+        }
+        if (lane == 31) scan[warp + 1] = upto;
+        __syncthreads();
+        int64_t before = upto - own, all = 0;
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+            if (w < warp) before += scan[w + 1];
+            all += scan[w + 1];
+        }
+        const int64_t piece = max(quotient(all + P.workers - 1, P.workers), (int64_t)1), from = piece * worker;
+        todo = min(piece, all - from);
+        if (todo > 0 && before <= from && from < before + own) {
+            int64_t left = from - before;
+            for (int i = s0; i < s1; ++i) {
+                const int64_t u = (int64_t)H * units_of[i];
+                if (left < u) { start_s = i; start_units = left; break; }
+                left -= u;
+            }
+        }
+        __syncthreads();
+        if (todo <= 0) {
+            if (tid == 0) P.cut[worker].units = 0;
+            return;
+        }
+        s = start_s;
+        q = wide_sequence(P, s);
+        head = (int)quotient(start_units, units_of[s]);
+        if (warp == 0) {
+            int left = (int)(start_units - (int64_t)head * units_of[s]);
+            for (int t0 = 0; t0 < q.tiles; t0 += 32) {
+                const int u = t0 + lane < q.tiles ? wide_tile(P, q, t0 + lane).units : 0;
+                int sum = u;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int v = __shfl_up_sync(~0u, sum, d);
+                    if (lane >= d) sum += v;
+                }
+                const unsigned hit = __ballot_sync(~0u, left < sum);
+                if (hit) {
+                    const int at = __ffs(hit) - 1;
+                    if (lane == at) { start_tile = t0 + at; start_unit = left - (sum - u); }
+                    break;
+                }
+                left -= __shfl_sync(~0u, sum, 31);
+            }
+        }
+        __syncthreads();
+        tile = start_tile;
+        skipped = start_unit;
+        first_unit = from - skipped;
+        if (tid == 0) {
+            Cut c;
+            c.first = first_unit; c.piece = piece;
+            c.units = wide_tile(P, q, tile).units; c.row = q.row; c.n = q.n; c.head = head; c.row0 = tile * kWideRows;
+            P.cut[worker] = c;
+        }
+    }
+
+    // ---- tensor memory (not before the launch ahead is done: it may want all of it)
+    if (warp == 0) {
+        tmem_alloc<false>(smem_at(&s_tmem), W::COLUMNS);
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem, my_lanes = (uint32_t)(warp * 32) << 16, t_scores = tmem, t_sums = tmem + TERMS * kWideUnit;
+    int *const timeout = P.status + 1;
+    const auto wait = [&](uint32_t bar, int &phase) {
+        mbar_wait<false>(bar, (uint32_t)(phase & 1), &s_abort, timeout, 2000000u);
+        ++phase;
+        __syncwarp();
+        tc_fence_after();
+    };
+    int phase_s = 0, phase_o = 0;
+    constexpr uint32_t IDESC_S = ((uint32_t)(kWideUnit >> 3) << 17) | (8u << 24) | (2u << 4) | (1u << 7) | (1u << 10);      // s8 s8 -> s32
+    constexpr uint32_t IDESC_O = ((uint32_t)(D >> 3) << 17) | (8u << 24) | (1u << 4) | (1u << 16);                          // f16 f16 (transposed) -> f32
+    const uint64_t q_desc = operand_desc(smem_at(qs), 128, D * 8), k_desc = operand_desc(smem_at(codes), 128, D * 8);
+    const uint64_t p_desc = operand_desc(smem_at(probs), 128, kWideUnit * 16), v_desc = operand_desc(smem_at(values), D * 16, 128);
+
+    bool whole = skipped == 0;
+    int slot = 0;
+    while (todo > 0) {
+        const WideTile w = wide_tile(P, q, tile);
+        const int row0 = tile * kWideRows, rows = min(kWideRows, q.n * G - row0), before = q.length - q.n;
+        // ---- queries, turned, as a factor times integers: eight rows of a warp at a time
+        {
+            constexpr int PAIRS = (D / 2 + 31) / 32, TOGETHER = D <= 128 ? 8 : 4;
+            for (int r0 = warp * 32; r0 < warp * 32 + 32; r0 += TOGETHER) {
+                float v[TOGETHER][2 * PAIRS];
+#pragma unroll
+                for (int k = 0; k < TOGETHER; ++k) {
+                    const int r = r0 + k, i = (row0 + r) / G;
+                    const T *const from = static_cast<const T *>(P.q) + (int64_t)(q.row + i) * P.q_stride + (int64_t)(head * G + (row0 + r) % G) * D;
+#pragma unroll
+                    for (int p = 0; p < PAIRS; ++p) {
+                        const int u = lane + 32 * p;
+                        const int2 at = pair_of(P.rotation, u);
+                        const bool in = r < rows && u < D / 2;
+                        v[k][2 * p] = in ? widen(from[at.x]) : 0.0f;
+                        v[k][2 * p + 1] = in ? widen(from[at.y]) : 0.0f;
+                    }
+                }
+                float2 by[PAIRS];
+                int turned_at = -1;                       // (the query heads of a row share its angles)
+#pragma unroll
+                for (int k = 0; k < TOGETHER; ++k) {
+                    const int r = r0 + k, i = (row0 + r) / G;
+                    if (r < rows && before + i >= 0) {
+                        if (i != turned_at) {
+                            turned_at = i;
+#pragma unroll
+                            for (int p = 0; p < PAIRS; ++p)
+                                if (lane + 32 * p < P.rotation.rotary / 2) by[p] = angle(P.rotation.freq[lane + 32 * p], before + i);
+                        }
+#pragma unroll
+                        for (int p = 0; p < PAIRS; ++p)
+                            if (lane + 32 * p < P.rotation.rotary / 2) turn(by[p], v[k][2 * p], v[k][2 * p + 1]);
+                    }
+                    unsigned most = 0;
+#pragma unroll
+                    for (int p = 0; p < 2 * PAIRS; ++p) most = max(most, __float_as_uint(v[k][p]) & 0x7FFFFFFFu);
+                    most = __reduce_max_sync(~0u, most);
+                    // (as in narrow_kernel)
+                    constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
+                    const bool finite = most < 0x7F800000u;
+                    const float top = fmaxf(__uint_as_float(most), 7.8886e-31f), scale = finite ? LIMIT / top : 0.0f;
+#pragma unroll
+                    for (int p = 0; p < PAIRS; ++p) {
+                        const int u = lane + 32 * p;
+                        if (u < D / 2) {
+                            const int2 at = pair_of(P.rotation, u);
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                int x = finite ? min(max(__float2int_rn(v[k][2 * p + j] * scale), -(int)LIMIT), (int)LIMIT) : 0;
+                                const int d = j ? at.y : at.x;
+                                int8_t *const to = qs + (r >> 3) * (D * 8) + (d >> 4) * 128 + (r & 7) * 16 + (d & 15);
+#pragma unroll
+                                for (int m = 0; m < TERMS; ++m) {
+                                    const int low = m == TERMS - 1 ? x : (int)(int8_t)x;
+                                    to[m * kWideRows * D] = (int8_t)low;
+                                    x = (x - low) >> 8;
+                                }
+                            }
+                        }
+                    }
+                    if (lane == 0) row_factor[r] = finite ? top / LIMIT * P.scale : NAN;
+                }
+            }
+        }
+
+        // ---- tokens: copies one step ahead
+        const int units = (int)min(todo, (int64_t)(w.units - skipped));
+        const bool last_part = skipped + units == w.units;
+        const int token_begin = w.from + (int)skipped * kWideUnit;
+        // lane l < 4 holds the page table's entry of the step's l-th 16 tokens
+        const auto entry_of = [&](int token) {
+            const int at = (token + lane * 16) >> P.cache.page_shift;
+            return lane < 4 && token + lane * 16 < w.to && at < P.batch.table_stride ? P.batch.table[(int64_t)s * P.batch.table_stride + at] : -2;
+        };
+        int entry = entry_of(token_begin), fetched = 0;
+        unsigned there[2] = {0, 0};                       // of a stage: which 16 tokens are in pages that are there
+        const auto fetch = [&](int stage) {
+            if (fetched < units) {
+                const int token = token_begin + fetched * kWideUnit;
+                const bool good = entry >= 0 && entry < P.cache.pages;
+                if (entry != -2 && !good && lane < 4 && warp == 0) atomicExch(P.status, 1);
+                there[stage] = __ballot_sync(~0u, good) & 15u;
+                const int64_t page = (int64_t)entry * H + head;
+                if (good && lane < 4 && warp < 2) copy_async4(smem_at(&stage_scale[stage][warp][lane]), P.cache.scale[warp] + page);
+                const uint32_t to = smem_at(codes) + stage * 2 * W::CODES;
+#pragma unroll
+                for (int i = 0; i < kWideUnit * CHUNKS / kWideThreads; ++i) {
+                    const int p = tid + kWideThreads * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
+                    const int e = __shfl_sync(~0u, entry, block >> 1), at = token + block * 8 + (p & 7);
+                    if (there[stage] >> (block >> 1) & 1) {
+                        const int64_t from = ((((int64_t)e * H + head) << P.cache.page_shift) + (at & (P.cache.page_tokens - 1))) * D + c * 16;
+                        const uint32_t place = to + block * (D * 8) + c * 128 + (p & 7) * 16;
+                        copy_async16(place, P.cache.codes[0] + from);
+                        copy_async16(place + W::CODES, P.cache.codes[1] + from);
+                    }
+                }
+                ++fetched;
+                entry = entry_of(token + kWideUnit);
+            }
+            copy_async_commit();
+        };
+        const auto scores = [&](int stage) {              // (one thread)
+            const uint32_t a0 = (uint32_t)q_desc, b0 = (uint32_t)k_desc + stage * 2 * W::CODES / 16;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int m = 0; m < TERMS; ++m)
+                    mma_i8<false>(t_scores + m * kWideUnit, a0 + m * (kWideRows * D / 16) + c * 16, (uint32_t)(q_desc >> 32), b0 + c * 16, (uint32_t)(k_desc >> 32), IDESC_S, c > 0);
+            tc_commit<false>(bar_s, 0);
+        };
+        fetch(0);
+        copy_async_wait<0>();
+        fence_async_proxy();
+        __syncthreads();
+        const float factor = row_factor[tid];
+        const int position = tid < rows ? before + (row0 + tid) / G : -1;
+        if (tid == 0) scores(0);
+        float m = -INFINITY, l = 0.0f, unit = 0.0f;
+#pragma unroll 1
+        for (int u = 0; u < units; ++u) {
+            const int stage = u & 1, token = token_begin + u * kWideUnit;
+            fetch(stage ^ 1);
+            if (u > 0) wait(bar_o, phase_o);              // the product before: values, probabilities and sums are free
+            // ---- values to fp16
+            {
+                const unsigned char *const from = codes + stage * 2 * W::CODES + W::CODES;
+#pragma unroll
+                for (int i = 0; i < kWideUnit * CHUNKS / kWideThreads; ++i) {
+                    const int p = tid + kWideThreads * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
+                    const uint4 r = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
+                    const uint32_t x[4] = {r.x ^ 0x80808080u, r.y ^ 0x80808080u, r.z ^ 0x80808080u, r.w ^ 0x80808080u};
+                    uint4 *const to = reinterpret_cast<uint4 *>(values + block * (D * 16) + c * 256 + (p & 7) * 16);
+                    to[0] = make_uint4(widen_codes<0x4140>(x[0]), widen_codes<0x4342>(x[0]), widen_codes<0x4140>(x[1]), widen_codes<0x4342>(x[1]));
+                    to[8] = make_uint4(widen_codes<0x4140>(x[2]), widen_codes<0x4342>(x[2]), widen_codes<0x4140>(x[3]), widen_codes<0x4342>(x[3]));
+                }
+            }
+            // ---- scores in powers of two
+            wait(bar_s, phase_s);
+            float sc[kWideUnit];
+#pragma unroll
+            for (int c = 0; c < kWideUnit / 16; ++c) {
+                uint32_t r[TERMS][16];
+#pragma unroll
+                for (int k = 0; k < TERMS; ++k) tmem_ld16(t_scores + my_lanes + k * kWideUnit + c * 16, r[k]);
+                tmem_wait_ld();
+                const float by = stage_scale[stage][0][c] * factor;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float low = (float)((int)r[1][i] * 256 + (int)r[0][i]);
+                    sc[c * 16 + i] = by * (TERMS == 3 ? fmaf((float)(int)r[TERMS - 1][i], 65536.0f, low) : low);
+                }
+            }
+            if (__any_sync(~0u, token + kWideUnit - 1 > position) || P.window > 0 || there[stage] != 15u) {
+#pragma unroll
+                for (int i = 0; i < kWideUnit; ++i)
+                    if (token + i > position || (P.window > 0 && token + i <= position - P.window) || !(there[stage] >> (i >> 4) & 1)) sc[i] = -INFINITY;
+            }
+            float most = sc[0];
+#pragma unroll
+            for (int i = 1; i < kWideUnit; ++i) most = max_or_nan(most, sc[i]);
+            // ---- the row's reference, the values' unit
+            float shrink = 1.0f;
+            if (!(most <= m + kFar)) {                    // (from -infinity too; a NaN stays)
+                shrink = exp2_approx(m - most);
+                m = most;
+            }
+            float by[4], top_scale = 0.0f;
+            unsigned odd = 0;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float v = stage_scale[stage][1][g];
+                by[g] = there[stage] >> g & 1 ? v : 0.0f;
+                if (!(by[g] < INFINITY)) { by[g] = 0.0f; odd |= 1u << g; }
+                top_scale = fmaxf(top_scale, by[g]);
+            }
+            l *= shrink;
+            if (top_scale > 2.0f * unit) {
+                shrink *= unit / top_scale;
+                unit = top_scale;
+            }
+            if (odd) {                                    // the rows that see some of a lost page are lost, the others are not
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (odd >> g & 1 && token + 16 * g <= position && (P.window == 0 || token + 16 * g + 15 > position - P.window)) l = NAN;
+            }
+            const float base = m == -INFINITY ? 0.0f : m, over = unit > 0.0f ? kWideLift / unit : 0.0f;
+            // ---- probabilities
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float lift = by[g] * over;
+                uint32_t hi[8], lo[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x0 = exp2_approx(sc[16 * g + 2 * i] - base), x1 = exp2_approx(sc[16 * g + 2 * i + 1] - base);
+                    l += x0 + x1;
+                    hi[i] = pack_half(x0 * lift, x1 * lift);
+                    if (W::SPLIT) {
+                        const __half2 h = *reinterpret_cast<const __half2 *>(&hi[i]);
+                        lo[i] = pack_half(x0 * lift - __low2float(h), x1 * lift - __high2float(h));
+                    }
+                }
+                uint4 *const to = reinterpret_cast<uint4 *>(probs + (tid >> 3) * (kWideUnit * 16) + g * 256 + (tid & 7) * 16);
+                to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                to[8] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+                if (W::SPLIT) {
+                    to[W::PROBS / 16] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                    to[W::PROBS / 16 + 8] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+                }
+            }
+            if (u > 0 && __any_sync(~0u, shrink != 1.0f)) {
+#pragma unroll 1
+                for (int c = 0; c < D / 16; ++c) {
+                    uint32_t r[16];
+                    tmem_ld16(t_sums + my_lanes + c * 16, r);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * shrink);
+                    tmem_st16(t_sums + my_lanes + c * 16, r);
+                }
+                tmem_wait_st();
+            }
+            copy_async_wait<0>();
+            fence_async_proxy();
+            tc_fence_before();
+            __syncthreads();
+            if (tid == 0) {
+                tc_fence_after();
+#pragma unroll
+                for (int k = 0; k < kWideUnit / 16; ++k)
+#pragma unroll
+                    for (int part = W::SPLIT ? 1 : 0; part >= 0; --part)
+                        mma_f16<false>(t_sums, (uint32_t)p_desc + part * (W::PROBS / 16) + k * 16, (uint32_t)(p_desc >> 32), (uint32_t)v_desc + k * (2 * D * 16 / 16),
+                                       (uint32_t)(v_desc >> 32), IDESC_O, u > 0 || k > 0 || part != (W::SPLIT ? 1 : 0));
+                tc_commit<false>(bar_o, 0);
+                if (u + 1 < units) scores(stage ^ 1);
+            }
+        }
+        wait(bar_o, phase_o);
+        todo -= units;
+
+        // ---- the tile's results: a row to a thread
+        const bool complete = whole && last_part;
+        const float by = complete ? (l == 0.0f ? 0.0f : unit / (l * kWideLift)) : 1.0f;
+        T *const y = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + tid) / G) * P.y_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
+        float *const part = P.partial + (((int64_t)worker * 2 + slot) * kWideRows + tid) * D;
+        const bool vec = ((uintptr_t)y & 15) == 0;
+#pragma unroll 1
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t r[16];
+            tmem_ld16(t_sums + my_lanes + c * 16, r);
+            tmem_wait_ld();
+            if (tid < rows) {
+                float x[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = by == 0.0f ? 0.0f : __uint_as_float(r[i]) * by;
+                if (!complete) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(part + c * 16)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                } else {
+                    T o[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = narrow<T>(x[i]);
+                    if (vec) {
+                        uint4 raw[sizeof(T)];
+                        memcpy(raw, o, sizeof o);
+#pragma unroll
+                        for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(y + c * 16)[i] = raw[i];
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) y[c * 16 + i] = o[i];
+                    }
+                }
+            }
+            __syncwarp();
+        }
+        if (!complete) P.stats[((int64_t)worker * 2 + slot) * kWideRows + tid] = make_float4(m, l, unit, 0.0f);
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (todo > 0) {
+            skipped = 0;
+            if (++tile >= q.tiles) {
+                tile = 0;
+                if (++head >= H) {
+                    head = 0;
+                    do q = wide_sequence(P, ++s); while (q.n == 0);
+                }
+            }
+            whole = true;
+            slot = 1;
+        }
+    }
+    let_next();
+    copy_async_wait<0>();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) tmem_free<false>(tmem, W::COLUMNS);
+}
+
+template <int DT, int D> static WideKernel wide_of() {
+    if constexpr (Wide<DT, D>::SHARED > 216 * 1024) return {nullptr, 0, 0};
+    else return {(const void *)wide_kernel<DT, D>, Wide<DT, D>::SHARED, Wide<DT, D>::BLOCKS};
+}
+template <int DT> static WideKernel wide_dt(int dim) {
+    switch (dim) {
+    case 32: return wide_of<DT, 32>();
+    case 64: return wide_of<DT, 64>();
+    case 96: return wide_of<DT, 96>();
+    case 128: return wide_of<DT, 128>();
+    case 192: return wide_of<DT, 192>();
+    default: return wide_of<DT, 256>();
+    }
+}
+WideKernel wide_kernel_for(xgen_dtype t, int dim) { return t == XGEN_F32 ? wide_dt<XGEN_F32>(dim) : wide_dt<XGEN_F16_F32ACC>(dim); }
+
+}  // namespace attention

@@ -49,18 +49,19 @@ inline bool overlap(const void *a, size_t an, const void *b, size_t bn) {
     return a && b && an && bn && x < y + bn && y < x + an;
 }
 
-// The stream's work done, whether the kernels left a mark at `mark` (which is taken away again).
-inline xgen_status take_status(int device, int *mark, void *stream) {
+// The stream's work done, whether the kernels left a mark at `mark` (marks[0]: an argument that does not fit; marks[1], where there are two: a
+// wait that ran out); marks are taken away again.
+inline xgen_status take_status(int device, int *marks, int count, void *stream) {
     OnDevice on(device);
-    int seen = 0;
-    if (!on.ok || cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess ||
-        cudaMemcpyAsync(&seen, mark, 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream) != cudaSuccess ||
-        cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess ||
-        (seen && (cudaMemsetAsync(mark, 0, 4, (cudaStream_t)stream) != cudaSuccess || cudaStreamSynchronize((cudaStream_t)stream) != cudaSuccess))) {
+    int seen[2] = {0, 0};
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (!on.ok || cudaStreamSynchronize(st) != cudaSuccess || cudaMemcpyAsync(seen, marks, 4 * count, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess ||
+        ((seen[0] || seen[1]) && (cudaMemsetAsync(marks, 0, 4 * count, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess))) {
         cudaGetLastError();
         return XGEN_ERR_CUDA;
     }
-    return seen ? XGEN_ERR_INVALID_ARG : XGEN_OK;
+    return seen[1] ? XGEN_ERR_TIMEOUT : seen[0] ? XGEN_ERR_INVALID_ARG : XGEN_OK;
 }
 inline size_t element_bytes(xgen_dtype t) { return t == XGEN_F32 ? 4 : 2; }
 
