@@ -1189,6 +1189,8 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     P.group = group; P.window = h->d.window;
     P.scale = (float)((double)h->d.softmax_scale * 1.4426950408889634);
     P.status = h->d_status; P.early = 16;
+    P.vec_q = (uintptr_t)q % 16 == 0 && q_stride * eb % 16 == 0;
+    P.vec_y = (uintptr_t)y % 16 == 0 && y_stride * eb % 16 == 0;
     P.launched = (route.eights ? 1 : 0) + (route.wide ? 1 : 0);
     OnDevice on(h->device);
     if (!on.ok) return XGEN_ERR_CUDA;

@@ -123,6 +123,7 @@ struct RunParams {
     void *y;
     int64_t q_stride, y_stride;
     int group, window;
+    bool vec_q, vec_y;               // rows of q, of y, start on multiples of 16 bytes
     float scale, lift;               // softmax scale times log2(e); what the kernel's probabilities are multiplied by
     float *partial;                  // [workers][2][rows of a tile][dim] sums
     float4 *stats;                   // [workers][2][rows of a tile]: maximum, total, unit of the sums
@@ -136,7 +137,7 @@ struct RunParams {
 // Rows of a sequence (with all query heads of a key head) up to which narrow_kernel takes it where both kernels are launched.
 constexpr int kNarrowMost = 16;
 // The kernel for many rows (attention_wide.cu): what one needs to launch it; no kernel where the block's memory would not do.
-constexpr int kWideRows = 128, kWideThreads = 128, kWideUnit = 64, kWideSequences = 1024;
+constexpr int kWideRows = 128, kWideThreads = kWideRows + 32, kWideUnit = 64, kWideSequences = 1024;
 struct WideKernel {
     const void *kernel;
     int shared, blocks;              // blocks: resident on an SM at once

@@ -8,8 +8,9 @@
 //     contiguous direction (the operand is given as transposed), and kind::f16 adds their product to the sums.
 // The sums are rescaled only where a row's maximum rises by more than 2^7 (or the values' scale doubles): probabilities are
 // lifted by 2^7, so that fp16 holds what that leaves.
-// The order of a step keeps the tensor cores fed: while the product of step j and the scores of step j + 1 run, back to back, the
-// threads widen the values of step j + 1; codes of step j + 2 are on their way.  Two blocks to an SM fill each other's gaps.
+// A warp of its own issues the matrix instructions, the product of step j and the scores of step j + 1 back to back; meanwhile the
+// threads widen the values of step j + 1 (each the codes that it copied itself, so they need not meet), and codes of step j + 2 are on
+// their way.  Two blocks to an SM fill each other's gaps.
 //
 // The work is cut into equal pieces as in attention.cu; units are counted tile by tile here, since a causal tile of an early row takes
 // few of them.
@@ -36,7 +37,7 @@ using patconv::tmem_st16;
 using patconv::tmem_wait_ld;
 using patconv::tmem_wait_st;
 
-constexpr int kW = 4;                                     // warps
+constexpr int kRowWarps = kWideRows / 32, kW = kRowWarps + 1;      // warps that own rows; the last one issues the matrix instructions
 constexpr float kFar = 7.0f;                              // (2^7 * 2^7 * 2, for values up to twice the unit, is within fp16)
 
 template <int DT, int D> struct Wide {
@@ -48,6 +49,10 @@ template <int DT, int D> struct Wide {
     static constexpr int PROBS = kWideRows * kWideUnit * 2;
     static constexpr int SHARED = Q + 4 * CODES + VALUES + PROBS * (SPLIT ? 2 : 1);
     static constexpr int COLUMNS = TERMS * kWideUnit + D <= 256 ? 256 : 512;
+    // Sums of two terms lose their lowest bits, so that what is left goes into 23: an error of at most what the query row's largest component
+    // times 1/256 (1/128) of a key step gives (fp16 queries would have up to 16 steps' worth in a sum of 128).
+    static constexpr int DROP = D <= 128 ? 7 : 8;
+    static constexpr int TABLE_ROW = (D < 64 ? D / 2 : 32) + 1;           // angles of a position, a step's pairs
     static constexpr int BLOCKS = COLUMNS == 256 && SHARED <= 104 * 1024 ? 2 : 1;
 };
 
@@ -83,17 +88,16 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     unsigned char *const codes = shared + W::Q;                             // [2 stages][keys, values][64 tokens][D], likewise
     unsigned char *const values = codes + 4 * W::CODES;                     // fp16 [8 tokens of 16 bytes][D/8][8]
     unsigned char *const probs = values + W::VALUES;                        // fp16 [128 rows][64 tokens], 8 rows of 16 bytes contiguous
-    __shared__ float stage_scale[2][2][4];
+    __shared__ float stage_scale[kRowWarps][2][2][4];                       // each warp's own: [stage][keys, values][16 tokens]
     __shared__ int units_of[kWideSequences];
     __shared__ int64_t scan[kW + 1], start_units;
     __shared__ int start_s, start_tile, start_unit;
-    __shared__ float row_factor[kWideRows];
-    __shared__ __align__(8) uint64_t bars[2];
+    __shared__ __align__(8) uint64_t bars[3];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int H = P.cache.heads, G = P.group, worker = blockIdx.x;
-    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]);
+    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]), bar_p = smem_at(&bars[2]);
     wait_before();
 
     // ---- this block's piece of the line of units: sequences, key heads, tiles, units
@@ -114,6 +118,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             s_abort = 0;
             mbar_init(bar_s, 1);
             mbar_init(bar_o, 1);
+            mbar_init(bar_p, kWideRows);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
@@ -184,7 +189,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     }
 
     // ---- tensor memory (not before the launch ahead is done: it may want all of it)
-    if (warp == 0) {
+    if (warp == kRowWarps) {
         tmem_alloc<false>(smem_at(&s_tmem), W::COLUMNS);
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -199,7 +204,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         __syncwarp();
         tc_fence_after();
     };
-    int phase_s = 0, phase_o = 0;
+    int phase_s = 0, phase_o = 0, phase_p = 0;
     constexpr uint32_t IDESC_S = ((uint32_t)(kWideUnit >> 3) << 17) | (8u << 24) | (2u << 4) | (1u << 7) | (1u << 10);      // s8 s8 -> s32
     constexpr uint32_t IDESC_O = ((uint32_t)(D >> 3) << 17) | (8u << 24) | (1u << 4) | (1u << 16);                          // f16 f16 (transposed) -> f32
     const uint64_t q_desc = operand_desc(smem_at(qs), 128, D * 8), k_desc = operand_desc(smem_at(codes), 128, D * 8);
@@ -210,283 +215,356 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     while (todo > 0) {
         const WideTile w = wide_tile(P, q, tile);
         const int row0 = tile * kWideRows, rows = min(kWideRows, q.n * G - row0), before = q.length - q.n;
-        // ---- queries, turned, as a factor times integers: eight rows of a warp at a time
-        {
-            constexpr int PAIRS = (D / 2 + 31) / 32, TOGETHER = D <= 128 ? 8 : 4;
-            for (int r0 = warp * 32; r0 < warp * 32 + 32; r0 += TOGETHER) {
-                float v[TOGETHER][2 * PAIRS];
-#pragma unroll
-                for (int k = 0; k < TOGETHER; ++k) {
-                    const int r = r0 + k, i = (row0 + r) / G;
-                    const T *const from = static_cast<const T *>(P.q) + (int64_t)(q.row + i) * P.q_stride + (int64_t)(head * G + (row0 + r) % G) * D;
-#pragma unroll
-                    for (int p = 0; p < PAIRS; ++p) {
-                        const int u = lane + 32 * p;
-                        const int2 at = pair_of(P.rotation, u);
-                        const bool in = r < rows && u < D / 2;
-                        v[k][2 * p] = in ? widen(from[at.x]) : 0.0f;
-                        v[k][2 * p + 1] = in ? widen(from[at.y]) : 0.0f;
-                    }
-                }
-                float2 by[PAIRS];
-                int turned_at = -1;                       // (the query heads of a row share its angles)
-#pragma unroll
-                for (int k = 0; k < TOGETHER; ++k) {
-                    const int r = r0 + k, i = (row0 + r) / G;
-                    if (r < rows && before + i >= 0) {
-                        if (i != turned_at) {
-                            turned_at = i;
-#pragma unroll
-                            for (int p = 0; p < PAIRS; ++p)
-                                if (lane + 32 * p < P.rotation.rotary / 2) by[p] = angle(P.rotation.freq[lane + 32 * p], before + i);
-                        }
-#pragma unroll
-                        for (int p = 0; p < PAIRS; ++p)
-                            if (lane + 32 * p < P.rotation.rotary / 2) turn(by[p], v[k][2 * p], v[k][2 * p + 1]);
-                    }
-                    unsigned most = 0;
-#pragma unroll
-                    for (int p = 0; p < 2 * PAIRS; ++p) most = max(most, __float_as_uint(v[k][p]) & 0x7FFFFFFFu);
-                    most = __reduce_max_sync(~0u, most);
-                    // (as in narrow_kernel)
-                    constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
-                    const bool finite = most < 0x7F800000u;
-                    const float top = fmaxf(__uint_as_float(most), 7.8886e-31f), scale = finite ? LIMIT / top : 0.0f;
-#pragma unroll
-                    for (int p = 0; p < PAIRS; ++p) {
-                        const int u = lane + 32 * p;
-                        if (u < D / 2) {
-                            const int2 at = pair_of(P.rotation, u);
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                int x = finite ? min(max(__float2int_rn(v[k][2 * p + j] * scale), -(int)LIMIT), (int)LIMIT) : 0;
-                                const int d = j ? at.y : at.x;
-                                int8_t *const to = qs + (r >> 3) * (D * 8) + (d >> 4) * 128 + (r & 7) * 16 + (d & 15);
-#pragma unroll
-                                for (int m = 0; m < TERMS; ++m) {
-                                    const int low = m == TERMS - 1 ? x : (int)(int8_t)x;
-                                    to[m * kWideRows * D] = (int8_t)low;
-                                    x = (x - low) >> 8;
-                                }
-                            }
-                        }
-                    }
-                    if (lane == 0) row_factor[r] = finite ? top / LIMIT * P.scale : NAN;
-                }
-            }
-        }
-
-        // ---- tokens: copies one step ahead
         const int units = (int)min(todo, (int64_t)(w.units - skipped));
         const bool last_part = skipped + units == w.units;
-        const int token_begin = w.from + (int)skipped * kWideUnit;
-        // lane l < 4 holds the page table's entry of the step's l-th 16 tokens
-        const auto entry_of = [&](int token) {
-            const int at = (token + lane * 16) >> P.cache.page_shift;
-            return lane < 4 && token + lane * 16 < w.to && at < P.batch.table_stride ? P.batch.table[(int64_t)s * P.batch.table_stride + at] : -2;
-        };
-        int entry = entry_of(token_begin), fetched = 0;
-        unsigned there[2] = {0, 0};                       // of a stage: which 16 tokens are in pages that are there
-        const auto fetch = [&](int stage) {
-            if (fetched < units) {
-                const int token = token_begin + fetched * kWideUnit;
-                const bool good = entry >= 0 && entry < P.cache.pages;
-                if (entry != -2 && !good && lane < 4 && warp == 0) atomicExch(P.status, 1);
-                there[stage] = __ballot_sync(~0u, good) & 15u;
-                const int64_t page = (int64_t)entry * H + head;
-                if (good && lane < 4 && warp < 2) copy_async4(smem_at(&stage_scale[stage][warp][lane]), P.cache.scale[warp] + page);
-                const uint32_t to = smem_at(codes) + stage * 2 * W::CODES;
+        float l = 0.0f, m = -INFINITY, unit = 0.0f;
+        if (warp == kRowWarps) {
+            // ---- matrix instructions: whenever the threads are done with a step (first: with the queries)
+            if (lane == 0) {
+                const uint32_t q_hi = (uint32_t)(q_desc >> 32), k_hi = (uint32_t)(k_desc >> 32), p_hi = (uint32_t)(p_desc >> 32), v_hi = (uint32_t)(v_desc >> 32);
+                for (int u = -1; u < units; ++u) {
+                    mbar_wait<false>(bar_p, (uint32_t)(phase_p & 1), &s_abort, timeout, 2000000u);
+                    ++phase_p;
+                    tc_fence_after();
+                    if (u >= 0) {
 #pragma unroll
-                for (int i = 0; i < kWideUnit * CHUNKS / kWideThreads; ++i) {
-                    const int p = tid + kWideThreads * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
-                    const int e = __shfl_sync(~0u, entry, block >> 1), at = token + block * 8 + (p & 7);
-                    if (there[stage] >> (block >> 1) & 1) {
-                        const int64_t from = ((((int64_t)e * H + head) << P.cache.page_shift) + (at & (P.cache.page_tokens - 1))) * D + c * 16;
-                        const uint32_t place = to + block * (D * 8) + c * 128 + (p & 7) * 16;
-                        copy_async16(place, P.cache.codes[0] + from);
-                        copy_async16(place + W::CODES, P.cache.codes[1] + from);
+                        for (int k = 0; k < kWideUnit / 16; ++k)
+#pragma unroll
+                            for (int part = W::SPLIT ? 1 : 0; part >= 0; --part)
+                                mma_f16<false>(t_sums, (uint32_t)p_desc + part * (W::PROBS / 16) + k * 16, p_hi, (uint32_t)v_desc + k * 2 * D, v_hi, IDESC_O,
+                                               u > 0 || k > 0 || part != (W::SPLIT ? 1 : 0));
+                        tc_commit<false>(bar_o, 0);
                     }
-                }
-                ++fetched;
-                entry = entry_of(token + kWideUnit);
-            }
-            copy_async_commit();
-        };
-        const auto scores = [&](int stage) {              // (one thread)
-            const uint32_t a0 = (uint32_t)q_desc, b0 = (uint32_t)k_desc + stage * 2 * W::CODES / 16;
+                    if (u + 1 < units) {
+                        const uint32_t b0 = (uint32_t)k_desc + ((u + 1) & 1) * 2 * W::CODES / 16;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c)
+                        for (int c = 0; c < D / 32; ++c)
 #pragma unroll
-                for (int m = 0; m < TERMS; ++m)
-                    mma_i8<false>(t_scores + m * kWideUnit, a0 + m * (kWideRows * D / 16) + c * 16, (uint32_t)(q_desc >> 32), b0 + c * 16, (uint32_t)(k_desc >> 32), IDESC_S, c > 0);
-            tc_commit<false>(bar_s, 0);
-        };
-        fetch(0);
-        copy_async_wait<0>();
-        fence_async_proxy();
-        __syncthreads();
-        const float factor = row_factor[tid];
-        const int position = tid < rows ? before + (row0 + tid) / G : -1;
-        if (tid == 0) scores(0);
-        float m = -INFINITY, l = 0.0f, unit = 0.0f;
-#pragma unroll 1
-        for (int u = 0; u < units; ++u) {
-            const int stage = u & 1, token = token_begin + u * kWideUnit;
-            fetch(stage ^ 1);
-            if (u > 0) wait(bar_o, phase_o);              // the product before: values, probabilities and sums are free
-            // ---- values to fp16
-            {
-                const unsigned char *const from = codes + stage * 2 * W::CODES + W::CODES;
-#pragma unroll
-                for (int i = 0; i < kWideUnit * CHUNKS / kWideThreads; ++i) {
-                    const int p = tid + kWideThreads * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
-                    const uint4 r = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
-                    const uint32_t x[4] = {r.x ^ 0x80808080u, r.y ^ 0x80808080u, r.z ^ 0x80808080u, r.w ^ 0x80808080u};
-                    uint4 *const to = reinterpret_cast<uint4 *>(values + block * (D * 16) + c * 256 + (p & 7) * 16);
-                    to[0] = make_uint4(widen_codes<0x4140>(x[0]), widen_codes<0x4342>(x[0]), widen_codes<0x4140>(x[1]), widen_codes<0x4342>(x[1]));
-                    to[8] = make_uint4(widen_codes<0x4140>(x[2]), widen_codes<0x4342>(x[2]), widen_codes<0x4140>(x[3]), widen_codes<0x4342>(x[3]));
-                }
-            }
-            // ---- scores in powers of two
-            wait(bar_s, phase_s);
-            float sc[kWideUnit];
-#pragma unroll
-            for (int c = 0; c < kWideUnit / 16; ++c) {
-                uint32_t r[TERMS][16];
-#pragma unroll
-                for (int k = 0; k < TERMS; ++k) tmem_ld16(t_scores + my_lanes + k * kWideUnit + c * 16, r[k]);
-                tmem_wait_ld();
-                const float by = stage_scale[stage][0][c] * factor;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float low = (float)((int)r[1][i] * 256 + (int)r[0][i]);
-                    sc[c * 16 + i] = by * (TERMS == 3 ? fmaf((float)(int)r[TERMS - 1][i], 65536.0f, low) : low);
-                }
-            }
-            if (__any_sync(~0u, token + kWideUnit - 1 > position) || P.window > 0 || there[stage] != 15u) {
-#pragma unroll
-                for (int i = 0; i < kWideUnit; ++i)
-                    if (token + i > position || (P.window > 0 && token + i <= position - P.window) || !(there[stage] >> (i >> 4) & 1)) sc[i] = -INFINITY;
-            }
-            float most = sc[0];
-#pragma unroll
-            for (int i = 1; i < kWideUnit; ++i) most = max_or_nan(most, sc[i]);
-            // ---- the row's reference, the values' unit
-            float shrink = 1.0f;
-            if (!(most <= m + kFar)) {                    // (from -infinity too; a NaN stays)
-                shrink = exp2_approx(m - most);
-                m = most;
-            }
-            float by[4], top_scale = 0.0f;
-            unsigned odd = 0;
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float v = stage_scale[stage][1][g];
-                by[g] = there[stage] >> g & 1 ? v : 0.0f;
-                if (!(by[g] < INFINITY)) { by[g] = 0.0f; odd |= 1u << g; }
-                top_scale = fmaxf(top_scale, by[g]);
-            }
-            l *= shrink;
-            if (top_scale > 2.0f * unit) {
-                shrink *= unit / top_scale;
-                unit = top_scale;
-            }
-            if (odd) {                                    // the rows that see some of a lost page are lost, the others are not
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    if (odd >> g & 1 && token + 16 * g <= position && (P.window == 0 || token + 16 * g + 15 > position - P.window)) l = NAN;
-            }
-            const float base = m == -INFINITY ? 0.0f : m, over = unit > 0.0f ? kWideLift / unit : 0.0f;
-            // ---- probabilities
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float lift = by[g] * over;
-                uint32_t hi[8], lo[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x0 = exp2_approx(sc[16 * g + 2 * i] - base), x1 = exp2_approx(sc[16 * g + 2 * i + 1] - base);
-                    l += x0 + x1;
-                    hi[i] = pack_half(x0 * lift, x1 * lift);
-                    if (W::SPLIT) {
-                        const __half2 h = *reinterpret_cast<const __half2 *>(&hi[i]);
-                        lo[i] = pack_half(x0 * lift - __low2float(h), x1 * lift - __high2float(h));
-                    }
-                }
-                uint4 *const to = reinterpret_cast<uint4 *>(probs + (tid >> 3) * (kWideUnit * 16) + g * 256 + (tid & 7) * 16);
-                to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                to[8] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
-                if (W::SPLIT) {
-                    to[W::PROBS / 16] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                    to[W::PROBS / 16 + 8] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
-                }
-            }
-            if (u > 0 && __any_sync(~0u, shrink != 1.0f)) {
-#pragma unroll 1
-                for (int c = 0; c < D / 16; ++c) {
-                    uint32_t r[16];
-                    tmem_ld16(t_sums + my_lanes + c * 16, r);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * shrink);
-                    tmem_st16(t_sums + my_lanes + c * 16, r);
-                }
-                tmem_wait_st();
-            }
-            copy_async_wait<0>();
-            fence_async_proxy();
-            tc_fence_before();
-            __syncthreads();
-            if (tid == 0) {
-                tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < kWideUnit / 16; ++k)
-#pragma unroll
-                    for (int part = W::SPLIT ? 1 : 0; part >= 0; --part)
-                        mma_f16<false>(t_sums, (uint32_t)p_desc + part * (W::PROBS / 16) + k * 16, (uint32_t)(p_desc >> 32), (uint32_t)v_desc + k * (2 * D * 16 / 16),
-                                       (uint32_t)(v_desc >> 32), IDESC_O, u > 0 || k > 0 || part != (W::SPLIT ? 1 : 0));
-                tc_commit<false>(bar_o, 0);
-                if (u + 1 < units) scores(stage ^ 1);
-            }
-        }
-        wait(bar_o, phase_o);
-        todo -= units;
-
-        // ---- the tile's results: a row to a thread
-        const bool complete = whole && last_part;
-        const float by = complete ? (l == 0.0f ? 0.0f : unit / (l * kWideLift)) : 1.0f;
-        T *const y = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + tid) / G) * P.y_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
-        float *const part = P.partial + (((int64_t)worker * 2 + slot) * kWideRows + tid) * D;
-        const bool vec = ((uintptr_t)y & 15) == 0;
-#pragma unroll 1
-        for (int c = 0; c < D / 16; ++c) {
-            uint32_t r[16];
-            tmem_ld16(t_sums + my_lanes + c * 16, r);
-            tmem_wait_ld();
-            if (tid < rows) {
-                float x[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = by == 0.0f ? 0.0f : __uint_as_float(r[i]) * by;
-                if (!complete) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(part + c * 16)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                } else {
-                    T o[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] = narrow<T>(x[i]);
-                    if (vec) {
-                        uint4 raw[sizeof(T)];
-                        memcpy(raw, o, sizeof o);
-#pragma unroll
-                        for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(y + c * 16)[i] = raw[i];
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) y[c * 16 + i] = o[i];
+                            for (int k = 0; k < TERMS; ++k)
+                                mma_i8<false>(t_scores + k * kWideUnit, (uint32_t)q_desc + k * (kWideRows * D / 16) + c * 16, q_hi, b0 + c * 16, k_hi, IDESC_S, c > 0);
+                        tc_commit<false>(bar_s, 0);
                     }
                 }
             }
             __syncwarp();
+        } else {
+            const auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWideRows) : "memory"); };      // the threads with rows
+            // ---- queries, turned, as a factor times integers: a row to a thread, once for its largest component and once for the integers; angles
+            // of the tile's positions by turns in a table
+            const int first_i = row0 / G, my_i = (row0 + tid) / G;
+            float factor;
+            {
+                float2 *const table = reinterpret_cast<float2 *>(codes);
+                const int pairs = P.rotation.rotary / 2, positions = (row0 + rows - 1) / G - first_i + 1;
+                const bool halves = pairs > 0 && !P.rotation.interleaved, any = halves && P.rotation.rotary % 16;
+                const T *const from = static_cast<const T *>(P.q) + (int64_t)(q.row + my_i) * P.q_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
+                int8_t *const to = qs + (tid >> 3) * (D * 8) + (tid & 7) * 16;
+                constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
+                float largest = 0.0f, by = 0.0f;
+                bool finite = true;
+#pragma unroll 1
+                for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+                    for (int p0 = 0; p0 < D / 2; p0 += 32) {
+                        if (p0 < pairs) {
+                            meet();                       // (what the table was is no longer needed)
+                            for (int e = tid; e < positions * 32; e += kWideRows)
+                                if (p0 + (e & 31) < pairs) table[(e >> 5) * W::TABLE_ROW + (e & 31)] = angle(P.rotation.freq[p0 + (e & 31)], before + first_i + (e >> 5));
+                            meet();
+                        }
+                        const float2 *const mine = table + (my_i - first_i) * W::TABLE_ROW - p0;
+#pragma unroll 1
+                        for (int it = p0 / 8; it < min(p0 / 8 + 4, D / 16); ++it) {       // 16 components: pairs 8 it .. 8 it + 7
+                            const bool apart = halves && 16 * it < P.rotation.rotary;
+                            const int at0 = apart ? 8 * it : 16 * it, at1 = apart ? 8 * it + pairs : 16 * it + 8;
+                            float v[16];
+                            if (tid >= rows) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[j] = 0.0f;
+                            } else if (P.vec_q && !any) {
+                                T e[16];
+                                constexpr int V = sizeof(T) / 2;
+                                uint4 raw[2 * V];
+#pragma unroll
+                                for (int j = 0; j < V; ++j) {
+                                    raw[j] = __ldg(reinterpret_cast<const uint4 *>(from + at0) + j);
+                                    raw[V + j] = __ldg(reinterpret_cast<const uint4 *>(from + at1) + j);
+                                }
+                                memcpy(e, raw, sizeof e);
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) v[j] = widen(e[j]);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const int2 at = apart ? pair_of(P.rotation, 8 * it + j) : make_int2(16 * it + 2 * j, 16 * it + 2 * j + 1);
+                                    const float x = widen(from[at.x]), y = widen(from[at.y]);
+                                    if (apart) { v[j] = x; v[8 + j] = y; }
+                                    else { v[2 * j] = x; v[2 * j + 1] = y; }
+                                }
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (8 * it + j < pairs && tid < rows) {
+                                    if (apart) turn(mine[8 * it + j], v[j], v[8 + j]);
+                                    else turn(mine[8 * it + j], v[2 * j], v[2 * j + 1]);
+                                }
+                            if (pass == 0) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) largest = max_or_nan(largest, fabsf(v[j]));
+                                continue;
+                            }
+                            uint32_t bytes[TERMS][4];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                int x = finite ? min(max(__float2int_rn(v[j] * by), -(int)LIMIT), (int)LIMIT) : 0;
+#pragma unroll
+                                for (int k = 0; k < TERMS; ++k) {          // lowest byte first
+                                    const int low = k == TERMS - 1 ? x : (int)(int8_t)x;
+                                    bytes[k][j >> 2] = j & 3 ? bytes[k][j >> 2] | (uint32_t)(low & 255) << (8 * (j & 3)) : (uint32_t)(low & 255);
+                                    x = (x - low) >> 8;
+                                }
+                            }
+#pragma unroll
+                            for (int k = 0; k < TERMS; ++k) {
+                                int8_t *const t = to + k * kWideRows * D;
+                                if (!apart) *reinterpret_cast<uint4 *>(t + it * 128) = make_uint4(bytes[k][0], bytes[k][1], bytes[k][2], bytes[k][3]);
+                                else if (!any) {
+                                    *reinterpret_cast<uint2 *>(t + (at0 >> 4) * 128 + (at0 & 15)) = make_uint2(bytes[k][0], bytes[k][1]);
+                                    *reinterpret_cast<uint2 *>(t + (at1 >> 4) * 128 + (at1 & 15)) = make_uint2(bytes[k][2], bytes[k][3]);
+                                } else {
+#pragma unroll
+                                    for (int j = 0; j < 8; ++j) {
+                                        const int2 at = pair_of(P.rotation, 8 * it + j);
+                                        t[(at.x >> 4) * 128 + (at.x & 15)] = (int8_t)(bytes[k][j >> 2] >> (8 * (j & 3)));
+                                        t[(at.y >> 4) * 128 + (at.y & 15)] = (int8_t)(bytes[k][2 + (j >> 2)] >> (8 * (j & 3)));
+                                    }
+                                }
+                            }
+                        }
+                    }
+                    if (pass == 0) {                      // (as in narrow_kernel)
+                        finite = largest < INFINITY;
+                        largest = fmaxf(largest, 7.8886e-31f);
+                        by = finite ? LIMIT / largest : 0.0f;
+                    }
+                }
+                factor = finite ? largest / LIMIT * P.scale : NAN;
+                meet();                                   // (the table's memory is the codes' from here on)
+            }
+
+            // ---- tokens: copies one step ahead
+            const int token_begin = w.from + (int)skipped * kWideUnit;
+            // lane l < 4 holds the page table's entry of the step's l-th 16 tokens
+            const auto entry_of = [&](int token) {
+                const int at = (token + lane * 16) >> P.cache.page_shift;
+                return lane < 4 && token + lane * 16 < w.to && at < P.batch.table_stride ? P.batch.table[(int64_t)s * P.batch.table_stride + at] : -2;
+            };
+            int entry = entry_of(token_begin), fetched = 0;
+            unsigned there = 0, there_next = 0;           // which 16 tokens of this step (of the next) are in pages that are there
+            const uint32_t my_place = smem_at(codes) + (tid >> 3) / CHUNKS * (D * 8) + (tid >> 3) % CHUNKS * 128 + (tid & 7) * 16;
+            const auto fetch = [&](int stage) {
+                if (fetched < units) {
+                    const int token = token_begin + fetched * kWideUnit;
+                    const bool good = entry >= 0 && entry < P.cache.pages;
+                    if (entry != -2 && !good && lane < 4 && warp == 0) atomicExch(P.status, 1);
+                    there_next = __ballot_sync(~0u, good) & 15u;
+                    const int64_t page = (int64_t)entry * H + head;
+                    const int64_t first = ((page << P.cache.page_shift) + ((token + lane * 16) & (P.cache.page_tokens - 1))) * D;      // of this lane's 16 tokens
+                    if (good) {
+                        copy_async4(smem_at(&stage_scale[warp][stage][0][lane]), P.cache.scale[0] + page);
+                        copy_async4(smem_at(&stage_scale[warp][stage][1][lane]), P.cache.scale[1] + page);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kWideUnit * CHUNKS / kWideRows; ++i) {
+                        const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS, g = block >> 1;
+                        const int64_t from = __shfl_sync(~0u, first, g) + ((block & 1) * 8 + (p & 7)) * D + c * 16;
+                        if (there_next >> g & 1) {
+                            const uint32_t place = (D & (D - 1)) == 0 ? my_place + i * (kWideRows * 16) : smem_at(codes) + block * (D * 8) + c * 128 + (p & 7) * 16;
+                            copy_async16(place + stage * 2 * W::CODES, P.cache.codes[0] + from);
+                            copy_async16(place + stage * 2 * W::CODES + W::CODES, P.cache.codes[1] + from);
+                        }
+                    }
+                    ++fetched;
+                    entry = entry_of(token + kWideUnit);
+                }
+                copy_async_commit();
+            };
+            const auto hand_over = [&] {                  // what this thread wrote, and what it copied, is the matrix instructions'
+                copy_async_wait<0>();
+                fence_async_proxy();
+                tc_fence_before();
+                patconv::mbar_arrive(bar_p);
+            };
+            fetch(0);
+            hand_over();
+            const int position = tid < rows ? before + my_i : -1;
+#pragma unroll 1
+            for (int u = 0; u < units; ++u) {
+                const int stage = u & 1, token = token_begin + u * kWideUnit;
+                there = there_next;
+                __syncwarp();                             // (scales that lanes of this warp copied)
+                float k_scale[4], v_scale[4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) { k_scale[g] = stage_scale[warp][stage][0][g]; v_scale[g] = stage_scale[warp][stage][1][g]; }
+                fetch(stage ^ 1);
+                if (u > 0) wait(bar_o, phase_o);          // the product before: values, probabilities and sums are free
+                // ---- values to fp16
+                {
+                    const unsigned char *const from = codes + stage * 2 * W::CODES + W::CODES;
+#pragma unroll
+                    for (int i = 0; i < kWideUnit * CHUNKS / kWideRows; ++i) {
+                        const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
+                        const uint4 r = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
+                        const uint32_t x[4] = {r.x ^ 0x80808080u, r.y ^ 0x80808080u, r.z ^ 0x80808080u, r.w ^ 0x80808080u};
+                        uint4 *const to = reinterpret_cast<uint4 *>(values + block * (D * 16) + c * 256 + (p & 7) * 16);
+                        to[0] = make_uint4(widen_codes<0x4140>(x[0]), widen_codes<0x4342>(x[0]), widen_codes<0x4140>(x[1]), widen_codes<0x4342>(x[1]));
+                        to[8] = make_uint4(widen_codes<0x4140>(x[2]), widen_codes<0x4342>(x[2]), widen_codes<0x4140>(x[3]), widen_codes<0x4342>(x[3]));
+                    }
+                }
+                // ---- scores in powers of two
+                wait(bar_s, phase_s);
+                float sc[kWideUnit];
+#pragma unroll
+                for (int c = 0; c < kWideUnit / 16; ++c) {
+                    uint32_t r[TERMS][16];
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) tmem_ld16(t_scores + my_lanes + k * kWideUnit + c * 16, r[k]);
+                    tmem_wait_ld();
+                    if constexpr (TERMS == 3) {
+                        const float by = k_scale[c] * factor;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            sc[c * 16 + i] = by * fmaf((float)(int)r[2][i], 65536.0f, (float)((int)r[1][i] * 256 + (int)r[0][i]));
+                    } else {
+                        // an integer of less than 23 bits as the low bits of 1.5 * 2^23 (a conversion would take the exponentials' unit)
+                        const float by = k_scale[c] * factor * (float)(1 << W::DROP), less = -12582912.0f * by;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            sc[c * 16 + i] = fmaf(__uint_as_float(0x4B400000u + ((int)r[0][i] >> W::DROP) + (r[1][i] << (8 - W::DROP))), by, less);
+                    }
+                }
+                if (__any_sync(~0u, token + kWideUnit - 1 > position) || P.window > 0 || there != 15u) {
+#pragma unroll
+                    for (int i = 0; i < kWideUnit; ++i)
+                        if (token + i > position || (P.window > 0 && token + i <= position - P.window) || !(there >> (i >> 4) & 1)) sc[i] = -INFINITY;
+                }
+                float most[4];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    most[g] = sc[16 * g];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) most[g] = max_or_nan(most[g], sc[16 * g + i]);
+                }
+                const float largest = max_or_nan(max_or_nan(most[0], most[1]), max_or_nan(most[2], most[3]));
+                // ---- the row's reference, the values' unit
+                float shrink = 1.0f;
+                if (!(largest <= m + kFar)) {             // (from -infinity too; a NaN stays in l)
+                    shrink = exp2_approx(m - largest);
+                    m = largest;
+                }
+                l *= shrink;
+                float top_scale = 0.0f;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    if (!(there >> g & 1)) v_scale[g] = 0.0f;
+                    if (!(v_scale[g] < INFINITY)) {       // the rows that see some of a lost page are lost, the others are not
+                        if (token + 16 * g <= position && (P.window == 0 || token + 16 * g + 15 > position - P.window)) l = NAN;
+                        v_scale[g] = 0.0f;
+                    }
+                    top_scale = fmaxf(top_scale, v_scale[g]);
+                }
+                if (top_scale > 2.0f * unit) {
+                    shrink *= unit / top_scale;
+                    unit = top_scale;
+                }
+                const float base = m == -INFINITY ? 0.0f : m, over = unit > 0.0f ? kWideLift / unit : 0.0f;
+                // ---- probabilities, lifted; totals are of the unlifted ones
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    // values of 2^-47 of the largest unit and less are nothing in fp16 (and their lift nothing to divide by)
+                    const bool none = !(v_scale[g] * over >= 1e-12f);
+                    const float lift = none ? 1.0f : v_scale[g] * over, off = log2f(lift) - base;
+                    uint32_t hi[8], lo[8];
+                    float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x0 = exp2_approx(sc[16 * g + 2 * i] + off), x1 = exp2_approx(sc[16 * g + 2 * i + 1] + off);
+                        sum0 += x0;
+                        sum1 += x1;
+                        hi[i] = pack_half(x0, x1);
+                        if (W::SPLIT) {
+                            const __half2 h = *reinterpret_cast<const __half2 *>(&hi[i]);
+                            lo[i] = pack_half(x0 - __low2float(h), x1 - __high2float(h));
+                        }
+                    }
+                    l += __fdividef(sum0 + sum1, lift);
+                    if (none) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) hi[i] = lo[i] = 0;
+                    }
+                    uint4 *const to = reinterpret_cast<uint4 *>(probs + (tid >> 3) * (kWideUnit * 16) + g * 256 + (tid & 7) * 16);
+                    to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    to[8] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+                    if (W::SPLIT) {
+                        to[W::PROBS / 16] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                        to[W::PROBS / 16 + 8] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+                    }
+                }
+                if (u > 0 && __any_sync(~0u, shrink != 1.0f)) {
+#pragma unroll 1
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t r[16];
+                        tmem_ld16(t_sums + my_lanes + c * 16, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * shrink);
+                        tmem_st16(t_sums + my_lanes + c * 16, r);
+                    }
+                    tmem_wait_st();
+                }
+                hand_over();
+            }
+            wait(bar_o, phase_o);
         }
-        if (!complete) P.stats[((int64_t)worker * 2 + slot) * kWideRows + tid] = make_float4(m, l, unit, 0.0f);
+        todo -= units;
+
+        if (warp < kRowWarps) {
+            // ---- the tile's results: a row to a thread
+            const bool complete = whole && last_part;
+            const float by = complete ? (l == 0.0f ? 0.0f : unit / (l * kWideLift)) : 1.0f;
+            T *const y = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + tid) / G) * P.y_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
+            float *const part = P.partial + (((int64_t)worker * 2 + slot) * kWideRows + tid) * D;
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t r[16];
+                tmem_ld16(t_sums + my_lanes + c * 16, r);
+                tmem_wait_ld();
+                if (tid < rows) {
+                    float x[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = by == 0.0f ? 0.0f : __uint_as_float(r[i]) * by;
+                    if (!complete) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(part + c * 16)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    } else {
+                        T o[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = narrow<T>(x[i]);
+                        if (P.vec_y) {
+                            uint4 raw[sizeof(T)];
+                            memcpy(raw, o, sizeof o);
+#pragma unroll
+                            for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(y + c * 16)[i] = raw[i];
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) y[c * 16 + i] = o[i];
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+            if (!complete) P.stats[((int64_t)worker * 2 + slot) * kWideRows + tid] = make_float4(m, l, unit, 0.0f);
+        }
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
@@ -507,7 +585,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     copy_async_wait<0>();
     tc_fence_before();
     __syncthreads();
-    if (warp == 0) tmem_free<false>(tmem, W::COLUMNS);
+    if (warp == kRowWarps) tmem_free<false>(tmem, W::COLUMNS);
 }
 
 template <int DT, int D> static WideKernel wide_of() {
