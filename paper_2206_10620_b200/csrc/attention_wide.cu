@@ -8,9 +8,9 @@
 //     contiguous direction (the operand is given as transposed), and kind::f16 adds their product to the sums.
 // The sums are rescaled only where a row's maximum rises by more than 2^7 (or the values' scale doubles): probabilities are
 // lifted by 2^7, so that fp16 holds what that leaves.
-// A warp of its own issues the matrix instructions, the product of step j and the scores of step j + 1 back to back; meanwhile the
-// threads widen the values of step j + 1 (each the codes that it copied itself, so they need not meet), and codes of step j + 2 are on
-// their way.  Two blocks to an SM fill each other's gaps.
+// A warp of its own copies the codes, two steps ahead, and issues the matrix instructions, the product of step j and the scores of step
+// j + 1 back to back; meanwhile the threads widen the values of step j + 1.  They meet that warp alone (barriers in shared memory), not
+// one another.  Two blocks to an SM fill each other's gaps.
 //
 // The work is cut into equal pieces as in attention.cu; units are counted tile by tile here, since a causal tile of an early row takes
 // few of them.
@@ -37,7 +37,7 @@ using patconv::tmem_st16;
 using patconv::tmem_wait_ld;
 using patconv::tmem_wait_st;
 
-constexpr int kRowWarps = kWideRows / 32, kW = kRowWarps + 1;      // warps that own rows; the last one issues the matrix instructions
+constexpr int kRowWarps = kWideRows / 32, kW = kRowWarps + 1;      // warps that own rows; the last one copies and issues
 constexpr float kFar = 7.0f;                              // (2^7 * 2^7 * 2, for values up to twice the unit, is within fp16)
 
 template <int DT, int D> struct Wide {
@@ -52,7 +52,7 @@ template <int DT, int D> struct Wide {
     // Sums of two terms lose their lowest bits, so that what is left goes into 23: an error of at most what the query row's largest component
     // times 1/256 (1/128) of a key step gives (fp16 queries would have up to 16 steps' worth in a sum of 128).
     static constexpr int DROP = D <= 128 ? 7 : 8;
-    static constexpr int TABLE_ROW = (D < 64 ? D / 2 : 32) + 1;           // angles of a position, a step's pairs
+    static constexpr int TABLE = D >= 128 ? 32 : 16;      // pairs whose angles are in the table at once
     static constexpr int BLOCKS = COLUMNS == 256 && SHARED <= 104 * 1024 ? 2 : 1;
 };
 
@@ -88,16 +88,17 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     unsigned char *const codes = shared + W::Q;                             // [2 stages][keys, values][64 tokens][D], likewise
     unsigned char *const values = codes + 4 * W::CODES;                     // fp16 [8 tokens of 16 bytes][D/8][8]
     unsigned char *const probs = values + W::VALUES;                        // fp16 [128 rows][64 tokens], 8 rows of 16 bytes contiguous
-    __shared__ float stage_scale[kRowWarps][2][2][4];                       // each warp's own: [stage][keys, values][16 tokens]
+    __shared__ float stage_scale[2][2][4];                                  // [stage][keys, values][16 tokens]
+    __shared__ unsigned stage_there[2];                                     // which 16 tokens of a stage are in pages that are there
     __shared__ int units_of[kWideSequences];
     __shared__ int64_t scan[kW + 1], start_units;
     __shared__ int start_s, start_tile, start_unit;
-    __shared__ __align__(8) uint64_t bars[3];
+    __shared__ __align__(8) uint64_t bars[5];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int H = P.cache.heads, G = P.group, worker = blockIdx.x;
-    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]), bar_p = smem_at(&bars[2]);
+    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]), bar_p = smem_at(&bars[2]), bar_c = smem_at(&bars[3]);
     wait_before();
 
     // ---- this block's piece of the line of units: sequences, key heads, tiles, units
@@ -119,6 +120,8 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             mbar_init(bar_s, 1);
             mbar_init(bar_o, 1);
             mbar_init(bar_p, kWideRows);
+            mbar_init(bar_c, 32);
+            mbar_init(bar_c + 8, 32);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
@@ -204,7 +207,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         __syncwarp();
         tc_fence_after();
     };
-    int phase_s = 0, phase_o = 0, phase_p = 0;
+    int phase_s = 0, phase_o = 0, phase_p = 0, phase_c = 0;      // (phase_c counts steps: two barriers in turn)
     constexpr uint32_t IDESC_S = ((uint32_t)(kWideUnit >> 3) << 17) | (8u << 24) | (2u << 4) | (1u << 7) | (1u << 10);      // s8 s8 -> s32
     constexpr uint32_t IDESC_O = ((uint32_t)(D >> 3) << 17) | (8u << 24) | (1u << 4) | (1u << 16);                          // f16 f16 (transposed) -> f32
     const uint64_t q_desc = operand_desc(smem_at(qs), 128, D * 8), k_desc = operand_desc(smem_at(codes), 128, D * 8);
@@ -219,13 +222,62 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         const bool last_part = skipped + units == w.units;
         float l = 0.0f, m = -INFINITY, unit = 0.0f;
         if (warp == kRowWarps) {
-            // ---- matrix instructions: whenever the threads are done with a step (first: with the queries)
-            if (lane == 0) {
-                const uint32_t q_hi = (uint32_t)(q_desc >> 32), k_hi = (uint32_t)(k_desc >> 32), p_hi = (uint32_t)(p_desc >> 32), v_hi = (uint32_t)(v_desc >> 32);
-                for (int u = -1; u < units; ++u) {
-                    mbar_wait<false>(bar_p, (uint32_t)(phase_p & 1), &s_abort, timeout, 2000000u);
-                    ++phase_p;
-                    tc_fence_after();
+            // ---- codes, two steps ahead; matrix instructions, whenever the threads are done with a step (first: with the queries)
+            const int token_begin = w.from + (int)skipped * kWideUnit;
+            // lane l < 4 holds the page table's entry of the next step's l-th 16 tokens
+            const auto entry_of = [&](int token) {
+                const int at = (token + lane * 16) >> P.cache.page_shift;
+                return lane < 4 && token + lane * 16 < w.to && at < P.batch.table_stride ? P.batch.table[(int64_t)s * P.batch.table_stride + at] : -2;
+            };
+            int entry = entry_of(token_begin), fetched = 0;
+            const uint32_t my_place = smem_at(codes) + (lane & 7) * 16;
+            const auto fetch = [&] {
+                if (fetched < units) {
+                    const int stage = (phase_c + fetched) & 1, token = token_begin + fetched * kWideUnit;
+                    const bool good = entry >= 0 && entry < P.cache.pages;
+                    if (entry != -2 && !good) atomicExch(P.status, 1);
+                    const unsigned there = __ballot_sync(~0u, good) & 15u;
+                    if (lane == 0) stage_there[stage] = there;
+                    const int64_t page = (int64_t)entry * H + head;
+                    const int64_t first = ((page << P.cache.page_shift) + ((token + lane * 16) & (P.cache.page_tokens - 1))) * D;      // of this lane's 16 tokens
+                    if (good) {
+                        copy_async4(smem_at(&stage_scale[stage][0][lane]), P.cache.scale[0] + page);
+                        copy_async4(smem_at(&stage_scale[stage][1][lane]), P.cache.scale[1] + page);
+                    }
+                    const uint32_t place0 = my_place + stage * 2 * W::CODES;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int64_t from = __shfl_sync(~0u, first, g) + (lane & 7) * D + (lane >> 3) * 16;
+                        if (!(there >> g & 1)) continue;
+                        const int8_t *const k = P.cache.codes[0] + from, *const v = P.cache.codes[1] + from;
+#pragma unroll
+                        for (int i = 0; i < 2 * ((CHUNKS + 3) / 4); ++i) {                 // 8 tokens x 4 pieces of 16 bytes at a time
+                            const int block = i & 1, c = (i >> 1) * 4 + (lane >> 3);
+                            const uint32_t place = place0 + (2 * g + block) * (D * 8) + c * 128;
+                            if (CHUNKS % 4 && c >= CHUNKS) continue;
+                            copy_async16(place, k + block * 8 * D + (i >> 1) * 64);
+                            copy_async16(place + W::CODES, v + block * 8 * D + (i >> 1) * 64);
+                        }
+                    }
+                    ++fetched;
+                    entry = entry_of(token + kWideUnit);
+                }
+                copy_async_commit();
+            };
+            const uint32_t q_hi = (uint32_t)(q_desc >> 32), k_hi = (uint32_t)(k_desc >> 32), p_hi = (uint32_t)(p_desc >> 32), v_hi = (uint32_t)(v_desc >> 32);
+            fetch();
+            fetch();
+            for (int u = -1; u < units; ++u) {
+                if (u + 1 < units) {                      // the next step's codes are there
+                    if (u < 0) copy_async_wait<1>(); else copy_async_wait<0>();
+                    fence_async_proxy();
+                    patconv::mbar_arrive(bar_c + 8 * ((phase_c + u + 1) & 1));
+                }
+                mbar_wait<false>(bar_p, (uint32_t)(phase_p & 1), &s_abort, timeout, 2000000u);
+                ++phase_p;
+                __syncwarp();
+                tc_fence_after();
+                if (lane == 0) {
                     if (u >= 0) {
 #pragma unroll
                         for (int k = 0; k < kWideUnit / 16; ++k)
@@ -236,7 +288,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         tc_commit<false>(bar_o, 0);
                     }
                     if (u + 1 < units) {
-                        const uint32_t b0 = (uint32_t)k_desc + ((u + 1) & 1) * 2 * W::CODES / 16;
+                        const uint32_t b0 = (uint32_t)k_desc + ((phase_c + u + 1) & 1) * 2 * W::CODES / 16;
 #pragma unroll
                         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
@@ -245,8 +297,10 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         tc_commit<false>(bar_s, 0);
                     }
                 }
+                __syncwarp();
+                if (u >= 0) fetch();                      // into the stage that this step leaves
             }
-            __syncwarp();
+            phase_c += units;
         } else {
             const auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWideRows) : "memory"); };      // the threads with rows
             // ---- queries, turned, as a factor times integers: a row to a thread, once for its largest component and once for the integers; angles
@@ -254,7 +308,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             const int first_i = row0 / G, my_i = (row0 + tid) / G;
             float factor;
             {
-                float2 *const table = reinterpret_cast<float2 *>(codes);
+                float2 *const table = reinterpret_cast<float2 *>(values);
                 const int pairs = P.rotation.rotary / 2, positions = (row0 + rows - 1) / G - first_i + 1;
                 const bool halves = pairs > 0 && !P.rotation.interleaved, any = halves && P.rotation.rotary % 16;
                 const T *const from = static_cast<const T *>(P.q) + (int64_t)(q.row + my_i) * P.q_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
@@ -265,39 +319,46 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
 #pragma unroll 1
                 for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll 1
-                    for (int p0 = 0; p0 < D / 2; p0 += 32) {
+                    for (int p0 = 0; p0 < D / 2; p0 += W::TABLE) {
+                        constexpr int ITEMS = W::TABLE / 8, V = sizeof(T) / 2;            // items of 16 components: pairs 8 it .. 8 it + 7
+                        uint4 raw[ITEMS][2 * V];
+                        if (P.vec_q && !any) {
+#pragma unroll
+                            for (int k = 0; k < ITEMS; ++k) {
+                                const int it = p0 / 8 + k, at0 = halves && 16 * it < P.rotation.rotary ? 8 * it : 16 * it;
+                                const int at1 = halves && 16 * it < P.rotation.rotary ? at0 + pairs : at0 + 8;
+#pragma unroll
+                                for (int j = 0; j < V; ++j) {
+                                    raw[k][j] = tid < rows ? __ldg(reinterpret_cast<const uint4 *>(from + at0) + j) : make_uint4(0, 0, 0, 0);
+                                    raw[k][V + j] = tid < rows ? __ldg(reinterpret_cast<const uint4 *>(from + at1) + j) : make_uint4(0, 0, 0, 0);
+                                }
+                            }
+                        }
                         if (p0 < pairs) {
                             meet();                       // (what the table was is no longer needed)
-                            for (int e = tid; e < positions * 32; e += kWideRows)
-                                if (p0 + (e & 31) < pairs) table[(e >> 5) * W::TABLE_ROW + (e & 31)] = angle(P.rotation.freq[p0 + (e & 31)], before + first_i + (e >> 5));
+                            for (int e = tid; e < positions * W::TABLE; e += kWideRows) {
+                                const int at = e / W::TABLE, j = e % W::TABLE;
+                                if (p0 + j < pairs) table[at * W::TABLE + (j ^ (at % W::TABLE))] = angle(P.rotation.freq[p0 + j], before + first_i + at);
+                            }
                             meet();
                         }
-                        const float2 *const mine = table + (my_i - first_i) * W::TABLE_ROW - p0;
-#pragma unroll 1
-                        for (int it = p0 / 8; it < min(p0 / 8 + 4, D / 16); ++it) {       // 16 components: pairs 8 it .. 8 it + 7
+                        const int my_at = my_i - first_i;
+#pragma unroll
+                        for (int k = 0; k < ITEMS; ++k) {
+                            const int it = p0 / 8 + k;
                             const bool apart = halves && 16 * it < P.rotation.rotary;
                             const int at0 = apart ? 8 * it : 16 * it, at1 = apart ? 8 * it + pairs : 16 * it + 8;
                             float v[16];
-                            if (tid >= rows) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = 0.0f;
-                            } else if (P.vec_q && !any) {
+                            if (P.vec_q && !any) {
                                 T e[16];
-                                constexpr int V = sizeof(T) / 2;
-                                uint4 raw[2 * V];
-#pragma unroll
-                                for (int j = 0; j < V; ++j) {
-                                    raw[j] = __ldg(reinterpret_cast<const uint4 *>(from + at0) + j);
-                                    raw[V + j] = __ldg(reinterpret_cast<const uint4 *>(from + at1) + j);
-                                }
-                                memcpy(e, raw, sizeof e);
+                                memcpy(e, raw[k], sizeof e);
 #pragma unroll
                                 for (int j = 0; j < 16; ++j) v[j] = widen(e[j]);
                             } else {
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
                                     const int2 at = apart ? pair_of(P.rotation, 8 * it + j) : make_int2(16 * it + 2 * j, 16 * it + 2 * j + 1);
-                                    const float x = widen(from[at.x]), y = widen(from[at.y]);
+                                    const float x = tid < rows ? widen(from[at.x]) : 0.0f, y = tid < rows ? widen(from[at.y]) : 0.0f;
                                     if (apart) { v[j] = x; v[8 + j] = y; }
                                     else { v[2 * j] = x; v[2 * j + 1] = y; }
                                 }
@@ -305,8 +366,9 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 if (8 * it + j < pairs && tid < rows) {
-                                    if (apart) turn(mine[8 * it + j], v[j], v[8 + j]);
-                                    else turn(mine[8 * it + j], v[2 * j], v[2 * j + 1]);
+                                    const float2 turn_by = table[my_at * W::TABLE + ((8 * k + j) ^ (my_at % W::TABLE))];
+                                    if (apart) turn(turn_by, v[j], v[8 + j]);
+                                    else turn(turn_by, v[2 * j], v[2 * j + 1]);
                                 }
                             if (pass == 0) {
 #pragma unroll
@@ -349,64 +411,26 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                     }
                 }
                 factor = finite ? largest / LIMIT * P.scale : NAN;
-                meet();                                   // (the table's memory is the codes' from here on)
+                meet();                                   // (the table's memory is the values' from here on)
             }
 
-            // ---- tokens: copies one step ahead
-            const int token_begin = w.from + (int)skipped * kWideUnit;
-            // lane l < 4 holds the page table's entry of the step's l-th 16 tokens
-            const auto entry_of = [&](int token) {
-                const int at = (token + lane * 16) >> P.cache.page_shift;
-                return lane < 4 && token + lane * 16 < w.to && at < P.batch.table_stride ? P.batch.table[(int64_t)s * P.batch.table_stride + at] : -2;
-            };
-            int entry = entry_of(token_begin), fetched = 0;
-            unsigned there = 0, there_next = 0;           // which 16 tokens of this step (of the next) are in pages that are there
-            const uint32_t my_place = smem_at(codes) + (tid >> 3) / CHUNKS * (D * 8) + (tid >> 3) % CHUNKS * 128 + (tid & 7) * 16;
-            const auto fetch = [&](int stage) {
-                if (fetched < units) {
-                    const int token = token_begin + fetched * kWideUnit;
-                    const bool good = entry >= 0 && entry < P.cache.pages;
-                    if (entry != -2 && !good && lane < 4 && warp == 0) atomicExch(P.status, 1);
-                    there_next = __ballot_sync(~0u, good) & 15u;
-                    const int64_t page = (int64_t)entry * H + head;
-                    const int64_t first = ((page << P.cache.page_shift) + ((token + lane * 16) & (P.cache.page_tokens - 1))) * D;      // of this lane's 16 tokens
-                    if (good) {
-                        copy_async4(smem_at(&stage_scale[warp][stage][0][lane]), P.cache.scale[0] + page);
-                        copy_async4(smem_at(&stage_scale[warp][stage][1][lane]), P.cache.scale[1] + page);
-                    }
-#pragma unroll
-                    for (int i = 0; i < kWideUnit * CHUNKS / kWideRows; ++i) {
-                        const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS, g = block >> 1;
-                        const int64_t from = __shfl_sync(~0u, first, g) + ((block & 1) * 8 + (p & 7)) * D + c * 16;
-                        if (there_next >> g & 1) {
-                            const uint32_t place = (D & (D - 1)) == 0 ? my_place + i * (kWideRows * 16) : smem_at(codes) + block * (D * 8) + c * 128 + (p & 7) * 16;
-                            copy_async16(place + stage * 2 * W::CODES, P.cache.codes[0] + from);
-                            copy_async16(place + stage * 2 * W::CODES + W::CODES, P.cache.codes[1] + from);
-                        }
-                    }
-                    ++fetched;
-                    entry = entry_of(token + kWideUnit);
-                }
-                copy_async_commit();
-            };
-            const auto hand_over = [&] {                  // what this thread wrote, and what it copied, is the matrix instructions'
-                copy_async_wait<0>();
+            const auto hand_over = [&] {                  // what this thread wrote is the matrix instructions'
                 fence_async_proxy();
                 tc_fence_before();
                 patconv::mbar_arrive(bar_p);
             };
-            fetch(0);
+            const int token_begin = w.from + (int)skipped * kWideUnit;
             hand_over();
             const int position = tid < rows ? before + my_i : -1;
 #pragma unroll 1
             for (int u = 0; u < units; ++u) {
-                const int stage = u & 1, token = token_begin + u * kWideUnit;
-                there = there_next;
-                __syncwarp();                             // (scales that lanes of this warp copied)
+                const int stage = phase_c & 1, token = token_begin + u * kWideUnit;
+                mbar_wait<false>(bar_c + 8 * stage, (uint32_t)(phase_c >> 1 & 1), &s_abort, timeout, 2000000u);
+                ++phase_c;
+                const unsigned there = stage_there[stage];
                 float k_scale[4], v_scale[4];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) { k_scale[g] = stage_scale[warp][stage][0][g]; v_scale[g] = stage_scale[warp][stage][1][g]; }
-                fetch(stage ^ 1);
+                for (int g = 0; g < 4; ++g) { k_scale[g] = stage_scale[stage][0][g]; v_scale[g] = stage_scale[stage][1][g]; }
                 if (u > 0) wait(bar_o, phase_o);          // the product before: values, probabilities and sums are free
                 // ---- values to fp16
                 {
