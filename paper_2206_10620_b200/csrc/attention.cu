@@ -1014,7 +1014,9 @@ static int64_t part_bytes(const xgen_attention_packed &h, int64_t workers, int64
 static int64_t narrow_bytes(const xgen_attention_packed &h, const Route &r) { return r.eights ? part_bytes(h, h.workers[r.eights - 1], 8 * r.eights) : 0; }
 static int64_t workspace_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
     const Route r = route_of(h, b);
-    return narrow_bytes(h, r) + (r.wide ? part_bytes(h, h.wide_workers, kWideRows) : 0);
+    if (!r.wide) return narrow_bytes(h, r);
+    const int64_t rows = b.rows * h.d.q_heads, terms = wide_kernel_for(h.d.dtype, h.d.head_dim).terms;
+    return narrow_bytes(h, r) + part_bytes(h, h.wide_workers, kWideRows) + (rows * terms * h.d.head_dim + rows * 4 + 255) / 256 * 256;
 }
 
 }  // namespace attention
@@ -1189,7 +1191,6 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     P.group = group; P.window = h->d.window;
     P.scale = (float)((double)h->d.softmax_scale * 1.4426950408889634);
     P.status = h->d_status; P.early = 16;
-    P.vec_q = (uintptr_t)q % 16 == 0 && q_stride * eb % 16 == 0;
     P.vec_y = (uintptr_t)y % 16 == 0 && y_stride * eb % 16 == 0;
     P.launched = (route.eights ? 1 : 0) + (route.wide ? 1 : 0);
     OnDevice on(h->device);
@@ -1211,7 +1212,12 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     if (route.eights) st = attend(k.narrow, k.combine, h->workers[route.eights - 1], k.rows, kThreads, k.shared, work);
     if (st == XGEN_OK && route.wide) {
         const WideKernel w = wide_kernel_for(h->d.dtype, h->d.head_dim);
-        st = attend(w.kernel, k.combine_wide, h->wide_workers, kWideRows, kWideThreads, w.shared, work + narrow_bytes(*h, route));
+        P.q_bytes = reinterpret_cast<int8_t *>(work + narrow_bytes(*h, route) + part_bytes(*h, h->wide_workers, kWideRows));
+        P.q_factor = reinterpret_cast<float *>(P.q_bytes + b->rows * h->d.q_heads * (int64_t)w.terms * h->d.head_dim);
+        const int64_t warps = b->rows * ((h->d.q_heads + kQueryHeads - 1) / kQueryHeads);
+        void *args[] = {&P};
+        st = launch(w.queries, dim3((unsigned)((warps + kQueryThreads / 32 - 1) / (kQueryThreads / 32))), dim3(kQueryThreads), 0, stream, args);
+        if (st == XGEN_OK) st = attend(w.kernel, k.combine_wide, h->wide_workers, kWideRows, kWideThreads, w.shared, work + narrow_bytes(*h, route));
     }
     return st;
 }

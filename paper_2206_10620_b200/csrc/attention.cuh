@@ -67,6 +67,25 @@ __device__ __forceinline__ float max_or_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+__device__ __forceinline__ float max_or_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// The sequence that a row belongs to, or ends before (the first one that ends behind it: 32 probes at a time); -1 behind the last.  Every
+// lane of the warp takes part.
+__device__ __forceinline__ int sequence_of_row(const Batch &B, int64_t row) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = B.sequences;
+    while (lo < hi) {
+        const int step = (hi - lo + 31) / 32, probe = lo + lane * step;
+        const unsigned behind = __ballot_sync(~0u, probe < hi && B.row_start[probe + 1] > row);
+        const int first = behind ? __ffs(behind) - 1 : min(32, (hi - lo + step - 1) / step);       // probes before it end at or before the row
+        if (behind) hi = min(hi, lo + first * step);
+        if (first > 0) lo += (first - 1) * step + 1;
+    }
+    return lo < B.sequences ? lo : -1;
+}
 // Two of the four codes of `r` (its signs flipped: 0 .. 255) as fp16: 1024 + code as bits, less 1152.
 template <int SELECT> __device__ __forceinline__ uint32_t widen_codes(uint32_t flipped) {
     const uint32_t b = __byte_perm(flipped, 0x64646464u, SELECT);
@@ -123,11 +142,13 @@ struct RunParams {
     void *y;
     int64_t q_stride, y_stride;
     int group, window;
-    bool vec_q, vec_y;               // rows of q, of y, start on multiples of 16 bytes
+    bool vec_y;                      // rows of y start on multiples of 16 bytes
     float scale, lift;               // softmax scale times log2(e); what the kernel's probabilities are multiplied by
     float *partial;                  // [workers][2][rows of a tile][dim] sums
     float4 *stats;                   // [workers][2][rows of a tile]: maximum, total, unit of the sums
     struct Cut *cut;                 // [workers]
+    int8_t *q_bytes;                 // wide_kernel: [kv_heads][rows * group][terms][dim]: the queries' integers, bytes of the lowest value first
+    float *q_factor;                 // [kv_heads][rows * group]: what they are multiples of, times the scale
     int workers, early;
     int launched;                    // how many kernels share the sequences: 1 (this one takes all) or 2
     int *status;
@@ -139,9 +160,10 @@ constexpr int kNarrowMost = 16;
 // The kernel for many rows (attention_wide.cu): what one needs to launch it; no kernel where the block's memory would not do.
 constexpr int kWideRows = 128, kWideThreads = kWideRows + 32, kWideUnit = 64, kWideSequences = 1024;
 struct WideKernel {
-    const void *kernel;
-    int shared, blocks;              // blocks: resident on an SM at once
+    const void *kernel, *queries;    // `queries` goes before it
+    int shared, blocks, terms;       // blocks: resident on an SM at once
 };
+constexpr int kQueryThreads = 256, kQueryHeads = 8;      // a warp of `queries` takes a row's kQueryHeads heads
 WideKernel wide_kernel_for(xgen_dtype t, int dim);
 
 }  // namespace attention

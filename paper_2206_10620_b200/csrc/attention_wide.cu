@@ -52,7 +52,6 @@ template <int DT, int D> struct Wide {
     // Sums of two terms lose their lowest bits, so that what is left goes into 23: an error of at most what the query row's largest component
     // times 1/256 (1/128) of a key step gives (fp16 queries would have up to 16 steps' worth in a sum of 128).
     static constexpr int DROP = D <= 128 ? 7 : 8;
-    static constexpr int TABLE = D >= 128 ? 32 : 16;      // pairs whose angles are in the table at once
     static constexpr int BLOCKS = COLUMNS == 256 && SHARED <= 104 * 1024 ? 2 : 1;
 };
 
@@ -302,118 +301,20 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             }
             phase_c += units;
         } else {
-            const auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWideRows) : "memory"); };      // the threads with rows
-            // ---- queries, turned, as a factor times integers: a row to a thread, once for its largest component and once for the integers; angles
-            // of the tile's positions by turns in a table
-            const int first_i = row0 / G, my_i = (row0 + tid) / G;
-            float factor;
+            // ---- queries: a thread copies its row's bytes (where there is no row, the last one's: what comes of it goes nowhere)
+            const int my_row = row0 + min(tid, rows - 1);
+            const int64_t flat = (int64_t)head * P.batch.rows * G + (int64_t)q.row * G + my_row;
+            const float factor = P.q_factor[flat];
             {
-                float2 *const table = reinterpret_cast<float2 *>(values);
-                const int pairs = P.rotation.rotary / 2, positions = (row0 + rows - 1) / G - first_i + 1;
-                const bool halves = pairs > 0 && !P.rotation.interleaved, any = halves && P.rotation.rotary % 16;
-                const T *const from = static_cast<const T *>(P.q) + (int64_t)(q.row + my_i) * P.q_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
-                int8_t *const to = qs + (tid >> 3) * (D * 8) + (tid & 7) * 16;
-                constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
-                float largest = 0.0f, by = 0.0f;
-                bool finite = true;
-#pragma unroll 1
-                for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll 1
-                    for (int p0 = 0; p0 < D / 2; p0 += W::TABLE) {
-                        constexpr int ITEMS = W::TABLE / 8, V = sizeof(T) / 2;            // items of 16 components: pairs 8 it .. 8 it + 7
-                        uint4 raw[ITEMS][2 * V];
-                        if (P.vec_q && !any) {
+                const int8_t *const from = P.q_bytes + flat * (TERMS * D);
+                const uint32_t to = smem_at(qs) + (tid >> 3) * (D * 8) + (tid & 7) * 16;
 #pragma unroll
-                            for (int k = 0; k < ITEMS; ++k) {
-                                const int it = p0 / 8 + k, at0 = halves && 16 * it < P.rotation.rotary ? 8 * it : 16 * it;
-                                const int at1 = halves && 16 * it < P.rotation.rotary ? at0 + pairs : at0 + 8;
+                for (int k = 0; k < TERMS; ++k)
 #pragma unroll
-                                for (int j = 0; j < V; ++j) {
-                                    raw[k][j] = tid < rows ? __ldg(reinterpret_cast<const uint4 *>(from + at0) + j) : make_uint4(0, 0, 0, 0);
-                                    raw[k][V + j] = tid < rows ? __ldg(reinterpret_cast<const uint4 *>(from + at1) + j) : make_uint4(0, 0, 0, 0);
-                                }
-                            }
-                        }
-                        if (p0 < pairs) {
-                            meet();                       // (what the table was is no longer needed)
-                            for (int e = tid; e < positions * W::TABLE; e += kWideRows) {
-                                const int at = e / W::TABLE, j = e % W::TABLE;
-                                if (p0 + j < pairs) table[at * W::TABLE + (j ^ (at % W::TABLE))] = angle(P.rotation.freq[p0 + j], before + first_i + at);
-                            }
-                            meet();
-                        }
-                        const int my_at = my_i - first_i;
-#pragma unroll
-                        for (int k = 0; k < ITEMS; ++k) {
-                            const int it = p0 / 8 + k;
-                            const bool apart = halves && 16 * it < P.rotation.rotary;
-                            const int at0 = apart ? 8 * it : 16 * it, at1 = apart ? 8 * it + pairs : 16 * it + 8;
-                            float v[16];
-                            if (P.vec_q && !any) {
-                                T e[16];
-                                memcpy(e, raw[k], sizeof e);
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) v[j] = widen(e[j]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    const int2 at = apart ? pair_of(P.rotation, 8 * it + j) : make_int2(16 * it + 2 * j, 16 * it + 2 * j + 1);
-                                    const float x = tid < rows ? widen(from[at.x]) : 0.0f, y = tid < rows ? widen(from[at.y]) : 0.0f;
-                                    if (apart) { v[j] = x; v[8 + j] = y; }
-                                    else { v[2 * j] = x; v[2 * j + 1] = y; }
-                                }
-                            }
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (8 * it + j < pairs && tid < rows) {
-                                    const float2 turn_by = table[my_at * W::TABLE + ((8 * k + j) ^ (my_at % W::TABLE))];
-                                    if (apart) turn(turn_by, v[j], v[8 + j]);
-                                    else turn(turn_by, v[2 * j], v[2 * j + 1]);
-                                }
-                            if (pass == 0) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) largest = max_or_nan(largest, fabsf(v[j]));
-                                continue;
-                            }
-                            uint32_t bytes[TERMS][4];
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                int x = finite ? min(max(__float2int_rn(v[j] * by), -(int)LIMIT), (int)LIMIT) : 0;
-#pragma unroll
-                                for (int k = 0; k < TERMS; ++k) {          // lowest byte first
-                                    const int low = k == TERMS - 1 ? x : (int)(int8_t)x;
-                                    bytes[k][j >> 2] = j & 3 ? bytes[k][j >> 2] | (uint32_t)(low & 255) << (8 * (j & 3)) : (uint32_t)(low & 255);
-                                    x = (x - low) >> 8;
-                                }
-                            }
-#pragma unroll
-                            for (int k = 0; k < TERMS; ++k) {
-                                int8_t *const t = to + k * kWideRows * D;
-                                if (!apart) *reinterpret_cast<uint4 *>(t + it * 128) = make_uint4(bytes[k][0], bytes[k][1], bytes[k][2], bytes[k][3]);
-                                else if (!any) {
-                                    *reinterpret_cast<uint2 *>(t + (at0 >> 4) * 128 + (at0 & 15)) = make_uint2(bytes[k][0], bytes[k][1]);
-                                    *reinterpret_cast<uint2 *>(t + (at1 >> 4) * 128 + (at1 & 15)) = make_uint2(bytes[k][2], bytes[k][3]);
-                                } else {
-#pragma unroll
-                                    for (int j = 0; j < 8; ++j) {
-                                        const int2 at = pair_of(P.rotation, 8 * it + j);
-                                        t[(at.x >> 4) * 128 + (at.x & 15)] = (int8_t)(bytes[k][j >> 2] >> (8 * (j & 3)));
-                                        t[(at.y >> 4) * 128 + (at.y & 15)] = (int8_t)(bytes[k][2 + (j >> 2)] >> (8 * (j & 3)));
-                                    }
-                                }
-                            }
-                        }
-                    }
-                    if (pass == 0) {                      // (as in narrow_kernel)
-                        finite = largest < INFINITY;
-                        largest = fmaxf(largest, 7.8886e-31f);
-                        by = finite ? LIMIT / largest : 0.0f;
-                    }
-                }
-                factor = finite ? largest / LIMIT * P.scale : NAN;
-                meet();                                   // (the table's memory is the values' from here on)
+                    for (int c = 0; c < CHUNKS; ++c) copy_async16(to + k * kWideRows * D + c * 128, from + k * D + c * 16);
+                copy_async_commit();
+                copy_async_wait<0>();
             }
-
             const auto hand_over = [&] {                  // what this thread wrote is the matrix instructions'
                 fence_async_proxy();
                 tc_fence_before();
@@ -421,7 +322,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             };
             const int token_begin = w.from + (int)skipped * kWideUnit;
             hand_over();
-            const int position = tid < rows ? before + my_i : -1;
+            const int position = before + my_row / G;
 #pragma unroll 1
             for (int u = 0; u < units; ++u) {
                 const int stage = phase_c & 1, token = token_begin + u * kWideUnit;
@@ -431,14 +332,21 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 float k_scale[4], v_scale[4];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) { k_scale[g] = stage_scale[stage][0][g]; v_scale[g] = stage_scale[stage][1][g]; }
-                if (u > 0) wait(bar_o, phase_o);          // the product before: values, probabilities and sums are free
                 // ---- values to fp16
                 {
                     const unsigned char *const from = codes + stage * 2 * W::CODES + W::CODES;
+                    constexpr int MINE = kWideUnit * CHUNKS / kWideRows;
+                    uint4 raw[MINE];                      // (all loads ahead of all stores, which could alias for all the compiler knows)
 #pragma unroll
-                    for (int i = 0; i < kWideUnit * CHUNKS / kWideRows; ++i) {
+                    for (int i = 0; i < MINE; ++i) {
                         const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
-                        const uint4 r = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
+                        raw[i] = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
+                    }
+                    if (u > 0) wait(bar_o, phase_o);      // the product before: values, probabilities and sums are free
+#pragma unroll
+                    for (int i = 0; i < MINE; ++i) {
+                        const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
+                        const uint4 r = raw[i];
                         const uint32_t x[4] = {r.x ^ 0x80808080u, r.y ^ 0x80808080u, r.z ^ 0x80808080u, r.w ^ 0x80808080u};
                         uint4 *const to = reinterpret_cast<uint4 *>(values + block * (D * 16) + c * 256 + (p & 7) * 16);
                         to[0] = make_uint4(widen_codes<0x4140>(x[0]), widen_codes<0x4342>(x[0]), widen_codes<0x4140>(x[1]), widen_codes<0x4342>(x[1]));
@@ -448,12 +356,18 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 // ---- scores in powers of two
                 wait(bar_s, phase_s);
                 float sc[kWideUnit];
+                constexpr int TOGETHER = TERMS == 3 ? 1 : 2;      // (loads are waited for all at once)
+                uint32_t rr[TOGETHER][TERMS][16];
 #pragma unroll
                 for (int c = 0; c < kWideUnit / 16; ++c) {
-                    uint32_t r[TERMS][16];
+                    if (c % TOGETHER == 0) {
 #pragma unroll
-                    for (int k = 0; k < TERMS; ++k) tmem_ld16(t_scores + my_lanes + k * kWideUnit + c * 16, r[k]);
-                    tmem_wait_ld();
+                        for (int j = 0; j < TOGETHER; ++j)
+#pragma unroll
+                            for (int k = 0; k < TERMS; ++k) tmem_ld16(t_scores + my_lanes + k * kWideUnit + (c + j) * 16, rr[j][k]);
+                        tmem_wait_ld();
+                    }
+                    const uint32_t (&r)[TERMS][16] = rr[c % TOGETHER];
                     if constexpr (TERMS == 3) {
                         const float by = k_scale[c] * factor;
 #pragma unroll
@@ -467,17 +381,24 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                             sc[c * 16 + i] = fmaf(__uint_as_float(0x4B400000u + ((int)r[0][i] >> W::DROP) + (r[1][i] << (8 - W::DROP))), by, less);
                     }
                 }
-                if (__any_sync(~0u, token + kWideUnit - 1 > position) || P.window > 0 || there != 15u) {
+                if (__any_sync(~0u, token + kWideUnit - 1 > position || token <= position - P.window && P.window > 0) || there != 15u) {
+                    // tokens [first, last] of the step, as bits; 16 at a time where a page is not there
+                    const int last = position - token, first = P.window > 0 ? last - P.window + 1 : 0;
+                    uint64_t seen = last >= kWideUnit - 1 ? ~0ull : last < 0 ? 0ull : (2ull << last) - 1;
+                    if (first > 0) seen = first >= kWideUnit ? 0ull : seen & ~0ull << first;
+                    uint32_t half[2] = {(uint32_t)seen, (uint32_t)(seen >> 32)};
 #pragma unroll
-                    for (int i = 0; i < kWideUnit; ++i)
-                        if (token + i > position || (P.window > 0 && token + i <= position - P.window) || !(there >> (i >> 4) & 1)) sc[i] = -INFINITY;
+                    for (int g = 0; g < 4; ++g)
+                        if (!(there >> g & 1)) half[g >> 1] &= g & 1 ? 0xFFFFu : 0xFFFF0000u;
+#pragma unroll
+                    for (int i = 0; i < kWideUnit; ++i) sc[i] = half[i >> 5] & 1u << (i & 31) ? sc[i] : -INFINITY;
                 }
                 float most[4];
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    most[g] = sc[16 * g];
+                    most[g] = max_or_nan(sc[16 * g], sc[16 * g + 1]);
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) most[g] = max_or_nan(most[g], sc[16 * g + i]);
+                    for (int i = 2; i < 16; i += 2) most[g] = max_or_nan(most[g], sc[16 * g + i], sc[16 * g + i + 1]);
                 }
                 const float largest = max_or_nan(max_or_nan(most[0], most[1]), max_or_nan(most[2], most[3]));
                 // ---- the row's reference, the values' unit
@@ -612,9 +533,73 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     if (warp == kRowWarps) tmem_free<false>(tmem, W::COLUMNS);
 }
 
+// The queries of all rows, turned, as a factor times integers: a warp takes a row and some of its heads, which share their angles.
+template <int DT, int D> __global__ void __launch_bounds__(kQueryThreads) query_kernel(const RunParams P) {
+    using T = typename Elem<DT>::T;
+    constexpr int TERMS = Wide<DT, D>::TERMS, PAIRS = (D / 2 + 31) / 32;
+    const int lane = threadIdx.x & 31, G = P.group, heads = P.cache.heads * G;
+    let_next();
+    wait_before();
+    const int per_row = (heads + kQueryHeads - 1) / kQueryHeads;
+    const int64_t warp = (int64_t)blockIdx.x * (kQueryThreads / 32) + (threadIdx.x >> 5);
+    const int64_t row = warp / per_row;
+    if (row >= P.batch.rows) return;
+    const int head0 = (int)(warp - row * per_row) * kQueryHeads, head1 = min(head0 + kQueryHeads, heads);
+    const int s = sequence_of_row(P.batch, row);
+    if (s < 0) return;
+    const Span sp = span_of(P.batch, s);
+    if (row < sp.row || (P.launched > 1 && sp.n * G <= kNarrowMost)) return;
+    const int position = length_of(P.batch, s) - sp.n + (int)(row - sp.row);       // (below 0: nothing will be seen)
+    const T *const from = static_cast<const T *>(P.q) + row * P.q_stride;
+    float2 by[PAIRS];
+#pragma unroll
+    for (int p = 0; p < PAIRS; ++p)
+        by[p] = lane + 32 * p < P.rotation.rotary / 2 ? angle(P.rotation.freq[lane + 32 * p], max(position, 0)) : make_float2(1.0f, 0.0f);
+#pragma unroll 2
+    for (int head = head0; head < head1; ++head) {
+        float v[2 * PAIRS];
+        float largest = 0.0f;
+#pragma unroll
+        for (int p = 0; p < PAIRS; ++p) {
+            const int u = lane + 32 * p;
+            const int2 at = pair_of(P.rotation, u);
+            v[2 * p] = u < D / 2 ? widen(from[head * D + at.x]) : 0.0f;
+            v[2 * p + 1] = u < D / 2 ? widen(from[head * D + at.y]) : 0.0f;
+            if (u < P.rotation.rotary / 2) turn(by[p], v[2 * p], v[2 * p + 1]);
+            largest = max_or_nan(largest, fabsf(v[2 * p]), fabsf(v[2 * p + 1]));
+        }
+        largest = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(largest)));
+        // (as in narrow_kernel)
+        constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
+        const bool finite = largest < INFINITY;
+        const float top = fmaxf(largest, 7.8886e-31f), scale = finite ? LIMIT / top : 0.0f;
+        const int64_t flat = ((int64_t)(head / G) * P.batch.rows + row) * G + head % G;
+        int8_t *const to = P.q_bytes + flat * (TERMS * D);
+#pragma unroll
+        for (int p = 0; p < PAIRS; ++p) {
+            const int u = lane + 32 * p;
+            if (u < D / 2) {
+                const int2 at = pair_of(P.rotation, u);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    int x = finite ? min(max(__float2int_rn(v[2 * p + j] * scale), -(int)LIMIT), (int)LIMIT) : 0;
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) {      // lowest byte first
+                        const int low = k == TERMS - 1 ? x : (int)(int8_t)x;
+                        to[k * D + (j ? at.y : at.x)] = (int8_t)low;
+                        x = (x - low) >> 8;
+                    }
+                }
+            }
+        }
+        if (lane == 0) P.q_factor[flat] = finite ? top / LIMIT * P.scale : NAN;
+    }
+}
+
 template <int DT, int D> static WideKernel wide_of() {
-    if constexpr (Wide<DT, D>::SHARED > 216 * 1024) return {nullptr, 0, 0};
-    else return {(const void *)wide_kernel<DT, D>, Wide<DT, D>::SHARED, Wide<DT, D>::BLOCKS};
+    using W = Wide<DT, D>;
+    if constexpr (W::SHARED > 216 * 1024) return {};
+    else return {(const void *)wide_kernel<DT, D>, (const void *)query_kernel<DT, D>, W::SHARED, W::BLOCKS, W::TERMS};
 }
 template <int DT> static WideKernel wide_dt(int dim) {
     switch (dim) {
