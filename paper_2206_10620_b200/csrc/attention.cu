@@ -848,30 +848,32 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
 
 // Joins the partial results of the tile that the cut before `worker` falls into, if that is the tile's first cut: four groups of threads
 // take the parts in turn.
-constexpr int kCombineThreads = 512, kGroups = 4, kGroup = kCombineThreads / kGroups;
+constexpr int kCombineThreads = 512, kGroups = 4, kGroup = kCombineThreads / kGroups, kCombineRows = 16;      // rows of a block
 template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const RunParams P) {
     using T = typename Elem<DT>::T;
-    __shared__ float4 row_stat[ROWS];                     // maximum, unit, factor of the sums
+    constexpr int MINE = ROWS < kCombineRows ? ROWS : kCombineRows;
+    __shared__ float4 row_stat[MINE];                     // maximum, unit, factor of the sums
     __shared__ float4 shares[kGroups - 1][kGroup];
-    const int worker = blockIdx.x + 1, tid = threadIdx.x;
+    const int worker = blockIdx.x + 1, first_row = blockIdx.y * MINE, tid = threadIdx.x;
     let_next();
     wait_before();
     const Cut c = P.cut[worker];
     const int64_t from = c.piece * worker;
     if (c.units == 0 || c.first == from || c.first < from - c.piece) return;      // no piece; the cut is between two tiles, or not the tile's first
-    const int rows = min(ROWS, c.n * P.group - c.row0);
+    const int rows = min(MINE, c.n * P.group - c.row0 - first_row);      // of this block's
+    if (rows <= 0) return;
     const int parts = (int)quotient(c.first + c.units - 1, (int)min(c.piece, (int64_t)INT_MAX)) - (worker - 1) + 1;
     // the first part is its worker's last tile (or all it has), the others are their workers' first
     const int64_t first_slot = (int64_t)(worker - 1) * 2 + (c.first <= from - c.piece ? 0 : 1), next_slot = (int64_t)worker * 2;
     auto slot_of = [&](int part) { return part == 0 ? first_slot : next_slot + 2 * (part - 1); };
     {
         // statistics of a row: some threads of one warp
-        constexpr int PER = kCombineThreads / ROWS > 32 ? 32 : kCombineThreads / ROWS;
+        constexpr int PER = 32;
         const int r = tid / PER, k = tid % PER;
-        if (r < ROWS) {
+        if (r < rows) {
             float top = -INFINITY, unit = 0.0f;
             for (int part = k; part < parts; part += PER) {
-                const float4 x = P.stats[slot_of(part) * ROWS + r];
+                const float4 x = P.stats[slot_of(part) * ROWS + first_row + r];
                 top = max_or_nan(top, x.x);
                 unit = fmaxf(unit, x.z);
             }
@@ -883,7 +885,7 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
             const float base = top == -INFINITY ? 0.0f : top;
             float total = 0.0f;
             for (int part = k; part < parts; part += PER) {
-                const float4 x = P.stats[slot_of(part) * ROWS + r];
+                const float4 x = P.stats[slot_of(part) * ROWS + first_row + r];
                 total += exp2_approx(x.x - base) * x.y;
             }
 #pragma unroll
@@ -892,21 +894,39 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
         }
     }
     __syncthreads();
+    const auto put = [&](int r, int at, float4 v) {
+        const float by = row_stat[r].z;
+        T *const to = static_cast<T *>(P.y) + (int64_t)(c.row + (c.row0 + first_row + r) / P.group) * P.y_stride +
+                      (int64_t)(c.head * P.group + (c.row0 + first_row + r) % P.group) * D + at;
+        const float4 y = by == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
+        to[0] = narrow<T>(y.x); to[1] = narrow<T>(y.y); to[2] = narrow<T>(y.z); to[3] = narrow<T>(y.w);
+    };
+    const auto add = [&](float4 &v, int part, int r, int at) {
+        const int64_t slot = slot_of(part);
+        const float4 x = P.stats[slot * ROWS + first_row + r];
+        const float4 o = *reinterpret_cast<const float4 *>(P.partial + (slot * ROWS + first_row + r) * D + at);
+        const float4 stat = row_stat[r];
+        const float f = x.z == 0.0f ? 0.0f : exp2_approx(x.x - stat.x) * (x.z / stat.y);
+        v.x += f * o.x; v.y += f * o.y; v.z += f * o.z; v.w += f * o.w;
+    };
+    if (parts <= kGroups) {                               // a thread adds up all parts of what it has
+#pragma unroll 2
+        for (int i = tid; i < rows * (D / 4); i += kCombineThreads) {
+            const int r = i / (D / 4), at = i % (D / 4) * 4;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int part = 0; part < parts; ++part) add(v, part, r, at);
+            put(r, at, v);
+        }
+        return;
+    }
     const int group = tid / kGroup, in_group = tid % kGroup;
     for (int i0 = 0; i0 < rows * (D / 4); i0 += kGroup) {
         const int i = i0 + in_group, r = i / (D / 4), at = i % (D / 4) * 4;
         const bool in = r < rows;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f), stat = v;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (in) {
-            stat = row_stat[r];
 #pragma unroll 4
-            for (int part = group; part < parts; part += kGroups) {
-                const int64_t slot = slot_of(part);
-                const float4 x = P.stats[slot * ROWS + r];
-                const float4 o = *reinterpret_cast<const float4 *>(P.partial + (slot * ROWS + r) * D + at);
-                const float f = x.z == 0.0f ? 0.0f : exp2_approx(x.x - stat.x) * (x.z / stat.y);
-                v.x += f * o.x; v.y += f * o.y; v.z += f * o.z; v.w += f * o.w;
-            }
+            for (int part = group; part < parts; part += kGroups) add(v, part, r, at);
         }
         if (group) shares[group - 1][in_group] = v;
         __syncthreads();
@@ -916,9 +936,7 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
                 const float4 x = shares[k][in_group];
                 v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
             }
-            T *const to = static_cast<T *>(P.y) + (int64_t)(c.row + (c.row0 + r) / P.group) * P.y_stride + (int64_t)(c.head * P.group + (c.row0 + r) % P.group) * D + at;
-            const float4 y = stat.z == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * stat.z, v.y * stat.z, v.z * stat.z, v.w * stat.z);
-            to[0] = narrow<T>(y.x); to[1] = narrow<T>(y.y); to[2] = narrow<T>(y.z); to[3] = narrow<T>(y.w);
+            put(r, at, v);
         }
         __syncthreads();
     }
@@ -1204,7 +1222,7 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
         P.cut = reinterpret_cast<Cut *>(P.stats + (int64_t)workers * 2 * rows);
         void *args[] = {&P};
         xgen_status r = launch(kernel, dim3(workers), dim3(threads), shared, stream, args);
-        if (r == XGEN_OK && workers > 1) r = launch(combine, dim3(workers - 1), dim3(kCombineThreads), 0, stream, args);
+        if (r == XGEN_OK && workers > 1) r = launch(combine, dim3(workers - 1, (rows + kCombineRows - 1) / kCombineRows), dim3(kCombineThreads), 0, stream, args);
         return r;
     };
     const Kernels k = kernels_for(h->d, route.eights ? route.eights : 1);

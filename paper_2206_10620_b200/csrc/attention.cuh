@@ -163,7 +163,7 @@ struct WideKernel {
     const void *kernel, *queries;    // `queries` goes before it
     int shared, blocks, terms;       // blocks: resident on an SM at once
 };
-constexpr int kQueryThreads = 256, kQueryHeads = 8;      // a warp of `queries` takes a row's kQueryHeads heads
+constexpr int kQueryThreads = 256, kQueryHeads = 4;      // a warp of `queries` takes a row's kQueryHeads heads
 WideKernel wide_kernel_for(xgen_dtype t, int dim);
 
 }  // namespace attention

@@ -533,11 +533,12 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     if (warp == kRowWarps) tmem_free<false>(tmem, W::COLUMNS);
 }
 
-// The queries of all rows, turned, as a factor times integers: a warp takes a row and some of its heads, which share their angles.
+// The queries of all rows, turned, as a factor times integers: a warp takes a row and some of its heads, which share their angles; a lane four
+// neighbouring pairs of a head, so that D/8 lanes make up a head and bytes leave four at a time.
 template <int DT, int D> __global__ void __launch_bounds__(kQueryThreads) query_kernel(const RunParams P) {
     using T = typename Elem<DT>::T;
-    constexpr int TERMS = Wide<DT, D>::TERMS, PAIRS = (D / 2 + 31) / 32;
-    const int lane = threadIdx.x & 31, G = P.group, heads = P.cache.heads * G;
+    constexpr int TERMS = Wide<DT, D>::TERMS, LANES = D <= 32 ? 4 : D <= 64 ? 8 : D <= 128 ? 16 : 32, AT_ONCE = 32 / LANES;
+    const int lane = threadIdx.x & 31, in_head = lane % LANES, G = P.group, heads = P.cache.heads * G;
     let_next();
     wait_before();
     const int per_row = (heads + kQueryHeads - 1) / kQueryHeads;
@@ -551,48 +552,66 @@ template <int DT, int D> __global__ void __launch_bounds__(kQueryThreads) query_
     if (row < sp.row || (P.launched > 1 && sp.n * G <= kNarrowMost)) return;
     const int position = length_of(P.batch, s) - sp.n + (int)(row - sp.row);       // (below 0: nothing will be seen)
     const T *const from = static_cast<const T *>(P.q) + row * P.q_stride;
-    float2 by[PAIRS];
+    // pairs u0 .. u0 + 3: components at x .. x + 3 and y .. y + 3 (halves), or x .. x + 7; any way where the rotation ends inside
+    const int u0 = 4 * in_head, pairs = P.rotation.rotary / 2;
+    const bool in = u0 < D / 2, halves = pairs > 0 && !P.rotation.interleaved;
+    const bool apart = halves && u0 < pairs, any = halves && pairs % 4;
+    const int x = apart ? u0 : 2 * u0, y = apart ? u0 + pairs : 2 * u0 + 4;
+    float2 by[4];
 #pragma unroll
-    for (int p = 0; p < PAIRS; ++p)
-        by[p] = lane + 32 * p < P.rotation.rotary / 2 ? angle(P.rotation.freq[lane + 32 * p], max(position, 0)) : make_float2(1.0f, 0.0f);
+    for (int j = 0; j < 4; ++j) by[j] = in && u0 + j < pairs ? angle(P.rotation.freq[u0 + j], max(position, 0)) : make_float2(1.0f, 0.0f);
 #pragma unroll 2
-    for (int head = head0; head < head1; ++head) {
-        float v[2 * PAIRS];
+    for (int head2 = head0; head2 < head1; head2 += AT_ONCE) {
+        const int head = head2 + lane / LANES;
+        const bool there = in && head < head1;
+        const auto component = [&](int j) {               // of the lane's eight: firsts of the pairs, then seconds
+            if (any) {
+                const int2 at = pair_of(P.rotation, u0 + (j & 3));
+                return j < 4 ? at.x : at.y;
+            }
+            return apart ? (j < 4 ? x + j : y + j - 4) : 2 * (u0 + (j & 3)) + (j >> 2);
+        };
+        float v[8];
         float largest = 0.0f;
 #pragma unroll
-        for (int p = 0; p < PAIRS; ++p) {
-            const int u = lane + 32 * p;
-            const int2 at = pair_of(P.rotation, u);
-            v[2 * p] = u < D / 2 ? widen(from[head * D + at.x]) : 0.0f;
-            v[2 * p + 1] = u < D / 2 ? widen(from[head * D + at.y]) : 0.0f;
-            if (u < P.rotation.rotary / 2) turn(by[p], v[2 * p], v[2 * p + 1]);
-            largest = max_or_nan(largest, fabsf(v[2 * p]), fabsf(v[2 * p + 1]));
+        for (int j = 0; j < 8; ++j) v[j] = there ? widen(from[head * D + component(j)]) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            turn(by[j], v[j], v[4 + j]);
+            largest = max_or_nan(largest, fabsf(v[j]), fabsf(v[4 + j]));
         }
-        largest = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(largest)));
+#pragma unroll
+        for (int d = 1; d < LANES; d <<= 1) largest = max_or_nan(largest, __shfl_xor_sync(~0u, largest, d));
         // (as in narrow_kernel)
         constexpr float LIMIT = TERMS == 3 ? 127.0f * 65536.0f : 127.0f * 256.0f;
         const bool finite = largest < INFINITY;
         const float top = fmaxf(largest, 7.8886e-31f), scale = finite ? LIMIT / top : 0.0f;
+        if (!there) continue;
         const int64_t flat = ((int64_t)(head / G) * P.batch.rows + row) * G + head % G;
         int8_t *const to = P.q_bytes + flat * (TERMS * D);
+        uint32_t bytes[TERMS][2];
 #pragma unroll
-        for (int p = 0; p < PAIRS; ++p) {
-            const int u = lane + 32 * p;
-            if (u < D / 2) {
-                const int2 at = pair_of(P.rotation, u);
+        for (int j = 0; j < 8; ++j) {
+            int n = finite ? min(max(__float2int_rn(v[j] * scale), -(int)LIMIT), (int)LIMIT) : 0;
+            // where the four are to leave together, their places in the word: halves in order, neighbours alternating
+            const int word = apart ? j >> 2 : (j & 3) >> 1, place = apart ? j & 3 : 2 * (j & 1) + (j >> 2);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    int x = finite ? min(max(__float2int_rn(v[2 * p + j] * scale), -(int)LIMIT), (int)LIMIT) : 0;
-#pragma unroll
-                    for (int k = 0; k < TERMS; ++k) {      // lowest byte first
-                        const int low = k == TERMS - 1 ? x : (int)(int8_t)x;
-                        to[k * D + (j ? at.y : at.x)] = (int8_t)low;
-                        x = (x - low) >> 8;
-                    }
-                }
+            for (int k = 0; k < TERMS; ++k) {              // lowest byte first
+                const int low = k == TERMS - 1 ? n : (int)(int8_t)n;
+                if (any) to[k * D + component(j)] = (int8_t)low;
+                if (j == 0) bytes[k][0] = bytes[k][1] = 0;
+                bytes[k][word] |= (uint32_t)(low & 255) << (8 * place);
+                n = (n - low) >> 8;
             }
         }
-        if (lane == 0) P.q_factor[flat] = finite ? top / LIMIT * P.scale : NAN;
+        if (!any) {
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) {
+                *reinterpret_cast<uint32_t *>(to + k * D + x) = bytes[k][0];
+                *reinterpret_cast<uint32_t *>(to + k * D + y) = bytes[k][1];
+            }
+        }
+        if (in_head == 0) P.q_factor[flat] = finite ? top / LIMIT * P.scale : NAN;
     }
 }
 
