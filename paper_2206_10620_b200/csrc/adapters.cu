@@ -1,38 +1,50 @@
 // libpatconv: low-rank adapters of many requests beside a shared product, for sm_100a, and their C ABI.
 //
-// out[r] = y[r] + s_a B_a (A_a x[r]).  One kernel does both products: a cluster of eight blocks takes up to ROWS rows of one
-// request.  Each block multiplies its eighth of the input features (the sums over features are joined through the blocks'
-// shared memory), then each computes its eighth of the output channels.  So an adapter's matrices are read by eight SMs side by
-// side even for a single row, nothing goes through memory in between, and there is one launch.
+// out[r] = y[r] + s_a B_a (A_a x[r]).  One kernel does both products: a cluster of eight blocks (four or two where there are many
+// clusters) takes up to ROWS rows of one request.  Each block multiplies its part of the input features (the sums over features are
+// joined through the blocks' shared memory), then each computes its part of the output channels.  So an adapter's matrices are read
+// by eight SMs side by side even for a single row, nothing goes through memory in between, and there is one launch.
 //
-// The operands of the matrix instructions come straight from memory: which feature is which index of a product's sum is free as
-// long as both operands agree, so a lane takes 16 contiguous bytes of a row of x and the same 16 bytes of the rows of A.
-// Which channel is which column is free too: a lane's sums are 8 contiguous channels of its rows, so y and out move
-// 16 bytes at a time.
+// Which feature is which index of a product's sum is free as long as both operands agree, so a lane takes 16 contiguous bytes of a
+// row of x, and the matrices are stored as the lanes take them.  Which channel is which column is free too: a lane's sums are 8
+// contiguous channels of its rows, so y and out move 16 bytes at a time.
+//
+// Few rows are bound by latency: a chain of a load, a product, two meetings of the cluster, a load, a product.  48 rows of 48
+// requests, 4096 features and channels, rank 16, fp16: 9.2 us (7.6 MB, 1.2 us at the memory's rate); one row 6.2 us.  Many rows
+// overlap the chains of the blocks on an SM: 4 requests of 4600 rows in all, the same sizes: rank 16 31 us, rank 64 45 us (18 us
+// for the bytes), rank 128 52 us.  With the adapters' operands in registers instead of shared memory these were 39, 55 and 90 us; with
+// clusters of eight 33, 53 and 85 us.  fp32, rank 64: 174 us, bound by the instructions that split numbers into tf32 parts (three
+// products each: 28 TFLOP/s).
 //
 // fp16: the inner sums are brought to fp16 with a power of two for each row, so that no magnitude is lost or overflows.  fp32:
-// three products of tf32 parts (high x high, high x low, low x high): what is dropped is 2^-22 of a product.
+// three products of tf32 parts (high x high, high x low, low x high): what is dropped is 2^-21 of a product at most.
 #include <climits>
 #include <cstring>
 #include <new>
 #include <vector>
 
 #include "adapters.h"
+#include "ptx.cuh"
 #include "serve.cuh"
 
 struct xgen_adapters_packed {
     xgen_adapters_desc d;
     int device;
+    int processors;
     int rp, kp, np;             // rank, features and channels as stored: rounded up, the rest zeros
-    void *d_a, *d_b;            // [adapters][rp][kp], [adapters][np][rp]
+    void *d_a, *d_b;            // [adapters][kp / block][rp][block], [adapters][np / 32][rp / block][4][32 lanes][16 bytes]: see Order
     float *d_scale;
     int *d_status;
 };
 
 namespace adapters {
 using namespace serve;
+using patconv::copy16;
+using patconv::copy_commit;
+using patconv::copy_wait;
+using patconv::smem_u32;
 
-constexpr int kCluster = 8, kThreads = 128, kWarps = 4;
+constexpr int kCluster = 8;                              // the most blocks of a cluster
 
 struct Params {
     const void *x, *y, *a, *b;
@@ -41,7 +53,7 @@ struct Params {
     const float *scale;
     int *status;
     int64_t x_stride, y_stride, out_stride;
-    int rows, requests, k, kp, n, np, rank, adapters;
+    int rows, requests, k, kp, n, np, rank, adapters, cluster;
     bool vec_x, vec_y, in_place;
 };
 
@@ -88,144 +100,304 @@ __device__ __forceinline__ void split_tf32(float x, uint32_t &hi, uint32_t &lo) 
     asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(rest));
 }
 
-// d += the products of one block of features: lane 4g + t holds elements t*E .. t*E + E - 1 of the block (E = 16 bytes' worth) of
-// rows g (x0) and g + 8 (x1) of one operand and of row g (w) of the other.
-template <int DT> __device__ __forceinline__ void mma_block(float (&d)[4], const uint4 &x0, const uint4 &x1, const uint4 &w);
-template <> __device__ __forceinline__ void mma_block<XGEN_F16_F32ACC>(float (&d)[4], const uint4 &x0, const uint4 &x1, const uint4 &w) {
-    const uint32_t a[4] = {x0.x, x1.x, x0.y, x1.y}, b[4] = {x0.z, x1.z, x0.w, x1.w};
-    mma16(d, a, w.x, w.y);
-    mma16(d, b, w.z, w.w);
-}
-__device__ __forceinline__ void mma_split(float (&d)[4], const float (&x)[4], float w0, float w1) {
-    uint32_t ah[4], al[4], bh[2], bl[2];
+// The same for several numbers at once, by cheap instructions where all are finite and not among the very largest: then no rest is
+// infinite or NaN.  (A rest has 12 bits beside its sign; the last one is lost where it has them all, 2^-23 of x at most.)
+template <int N> __device__ __forceinline__ void split_tf32(const float (&x)[N], uint32_t (&hi)[N], uint32_t (&lo)[N]) {
+    float check = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) split_tf32(x[i], ah[i], al[i]);
-    split_tf32(w0, bh[0], bl[0]);
-    split_tf32(w1, bh[1], bl[1]);
-    mma_tf32(d, al, bh[0], bh[1]);
-    mma_tf32(d, ah, bl[0], bl[1]);
-    mma_tf32(d, ah, bh[0], bh[1]);
+    for (int i = 0; i < N; ++i) {
+        hi[i] = (__float_as_uint(x[i]) + 0x1000u) & 0xFFFFE000u;
+        const float rest = x[i] - __uint_as_float(hi[i]);
+        lo[i] = __float_as_uint(rest) & 0xFFFFE000u;
+        check += rest;
+    }
+    if (__any_sync(~0u, !(fabsf(check) < INFINITY))) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) split_tf32(x[i], hi[i], lo[i]);
+    }
 }
-template <> __device__ __forceinline__ void mma_block<XGEN_F32>(float (&d)[4], const uint4 &x0, const uint4 &x1, const uint4 &w) {
-    const float a[4] = {__uint_as_float(x0.x), __uint_as_float(x1.x), __uint_as_float(x0.y), __uint_as_float(x1.y)};
-    const float b[4] = {__uint_as_float(x0.z), __uint_as_float(x1.z), __uint_as_float(x0.w), __uint_as_float(x1.w)};
-    mma_split(d, a, __uint_as_float(w.x), __uint_as_float(w.y));
-    mma_split(d, b, __uint_as_float(w.z), __uint_as_float(w.w));
+
+// The left operand of one block of features: lane 4g + t holds elements t*E .. t*E + E - 1 of the block (E = 16 bytes' worth) of
+// rows g (x0) and g + 8 (x1); mma_block adds its products with row g of the right one (w) to d.
+template <int DT> struct Left {
+    uint32_t a[4], b[4];
+    __device__ __forceinline__ Left(const uint4 &x0, const uint4 &x1) : a{x0.x, x1.x, x0.y, x1.y}, b{x0.z, x1.z, x0.w, x1.w} {}
+};
+template <> struct Left<XGEN_F32> {
+    uint32_t hi[8], lo[8];
+    __device__ __forceinline__ Left(const uint4 &x0, const uint4 &x1) {
+        const float x[8] = {__uint_as_float(x0.x), __uint_as_float(x1.x), __uint_as_float(x0.y), __uint_as_float(x1.y),
+                            __uint_as_float(x0.z), __uint_as_float(x1.z), __uint_as_float(x0.w), __uint_as_float(x1.w)};
+        split_tf32(x, hi, lo);
+    }
+};
+__device__ __forceinline__ void mma_block(float (&d)[4], const Left<XGEN_F16_F32ACC> &x, const uint4 &w) {
+    mma16(d, x.a, w.x, w.y);
+    mma16(d, x.b, w.z, w.w);
+}
+__device__ __forceinline__ void mma_block(float (&d)[4], const Left<XGEN_F32> &x, const uint4 &w) {
+    const float v[4] = {__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w)};
+    uint32_t hi[4], lo[4];
+    split_tf32(v, hi, lo);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t ah[4] = {x.hi[4 * i], x.hi[4 * i + 1], x.hi[4 * i + 2], x.hi[4 * i + 3]};
+        const uint32_t al[4] = {x.lo[4 * i], x.lo[4 * i + 1], x.lo[4 * i + 2], x.lo[4 * i + 3]};
+        mma_tf32(d, al, hi[2 * i], hi[2 * i + 1]);
+        mma_tf32(d, ah, lo[2 * i], lo[2 * i + 1]);
+        mma_tf32(d, ah, hi[2 * i], hi[2 * i + 1]);
+    }
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ float far_load(const float *p, int rank) {
+__device__ __forceinline__ float4 far_load(const float *p, int rank) {
     uint32_t a;
-    float v;
+    float4 v;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
     return v;
 }
 
-// DT: type.  RP: rank as stored.  ROWS: 16 (the warps divide a block's features and channels among them) or 64 (16 rows each).
-template <int DT, int RP, int ROWS> __global__ void __launch_bounds__(kThreads) adapters_kernel(const Params P) {
+__device__ __forceinline__ float4 operator+(const float4 &a, const float4 &b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+
+// How the matrices are stored: in the order in which the lanes of a warp take them, 16 bytes each, so that a load of a warp is one
+// piece of 512 bytes.  (Strided rows, 64 bytes of each, take the L1 twice as long: 4600 rows at rank 128 took 162 us, 133 in this order.)
+template <int DT, int RP> struct Order {
+    static constexpr int E = DT == XGEN_F32 ? 4 : 8, BLOCK = 4 * E;
+    static constexpr bool HALF = RP < BLOCK;                            // (rank 16 in fp16: a lane's 16 bytes are 8 of each of two columns)
+    static constexpr int STEPS = HALF ? 1 : RP / BLOCK, LOADS = HALF ? 2 : 4;
+};
+
+// Many rows: the four warps of a group (64 rows) share the operands of an adapter; a step of theirs is a block of features (the inner
+// sums) or of 32 channels (the outer product).  DEPTH steps lie in shared memory: the adapter's part, then each warp's own rows.
+template <int DT, int RP> struct Ring {
+    using O = Order<DT, RP>;
+    static constexpr int DEPTH = 3, PIECES = 16 / O::E;                 // a warp's rows: so many times 512 bytes
+    static constexpr int SHARED = RP / 8 > O::STEPS * O::LOADS ? RP / 8 : O::STEPS * O::LOADS;
+    static constexpr int SLOT = (SHARED + 4 * PIECES) * 32;             // x 16 bytes
+    static constexpr int BYTES = 2 * DEPTH * SLOT * 16;
+};
+__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory"); }
+
+// Blocks that an SM holds at once: as many as can have the registers without spilling more than a few.
+constexpr int resident(int dt, int rp, bool wide) {
+    return dt == XGEN_F32 ? (rp <= 16 ? (wide ? 3 : 4) : rp <= 32 ? (wide ? 2 : 3) : wide ? (rp <= 64 ? 2 : 1) : rp <= 64 ? 3 : 2)
+                          : wide ? (rp <= 32 ? 4 : rp <= 64 ? 3 : 2) : rp <= 16 ? 6 : rp <= 32 ? 5 : rp <= 64 ? 3 : 2;
+}
+
+// DT: type.  RP: rank as stored.  ROWS: 16 (four warps divide a block's features and channels among them) or 64 (two warps to 16
+// rows divide theirs).
+template <int DT, int RP, int ROWS> __global__ void __launch_bounds__(ROWS == 64 ? 256 : 128, resident(DT, RP, ROWS == 64)) adapters_kernel(const Params P) {
     using T = typename Elem<DT>::T;
-    constexpr int E = 16 / sizeof(T), BLOCK = 4 * E, NT = RP / 8;
-    constexpr bool WIDE = ROWS == 64;
-    __shared__ __align__(16) float part[64 * RP];        // [warp][16][RP]: this block's share of the inner sums
-    __shared__ __align__(16) float total[WIDE ? 64 * RP / kCluster : 1];
+    using O = Order<DT, RP>;
+    constexpr int E = O::E, BLOCK = O::BLOCK, NT = RP / 8;
+    constexpr bool WIDE = ROWS == 64, HALF = O::HALF;
+    constexpr int kThreads = WIDE ? 256 : 128, GROUPS = ROWS / 16, SHARE = kThreads / 32 / GROUPS;  // SHARE: warps that have the same rows
+    using R = Ring<DT, RP>;
+    constexpr int DEPTH = R::DEPTH;
+    // few rows: a block of an adapter's operands is asked for while the one before is multiplied, as far as registers go
+    constexpr bool AHEAD_IN = !WIDE && NT <= 8, AHEAD_OUT = !WIDE && RP * (int)sizeof(T) <= 128;
+    extern __shared__ uint4 ring_of_all[];
+    __shared__ __align__(16) float part[64 * RP];        // [16 rows][RP] four times: this block's share of the inner sums
     __shared__ float row_scale[ROWS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int rank = (int)(blockIdx.x % kCluster);
+    const int C = P.cluster, rank = (int)blockIdx.x % C;
     let_next();
     wait_before();
-    const Tile tile = find_tile<ROWS>(P, (int)(blockIdx.x / kCluster));
+    const Tile tile = find_tile<ROWS>(P, (int)blockIdx.x / C);
     if (tile.count == 0) return;                         // (the whole cluster alike)
     int who = P.adapter[tile.request];
     if (who >= P.adapters) {
         if (tid == 0) atomicExch(P.status, 1);
         who = -1;
     }
-    const int row0 = WIDE ? warp * 16 : 0;               // of the tile, where this warp's 16 rows begin
+    // of the tile, where this warp's rows begin; which of the warps with the same rows it is
+    const int row0 = warp % GROUPS * 16, turn = warp / GROUPS;
+    uint4 *const ring = ring_of_all + turn * DEPTH * R::SLOT + lane;
+    const int own = (R::SHARED + warp % 4 * R::PIECES) * 32;               // in a slot: (each lane reads what it copied itself)
     const T *const y = static_cast<const T *>(P.y) + (int64_t)tile.row * P.y_stride;
     T *const out = static_cast<T *>(P.out) + (int64_t)tile.row * P.out_stride;
     const int blocks_n = P.np / 32;
 
     if (who < 0) {                                       // (the same for the whole cluster)
         if (P.in_place) return;
-        for (int64_t i = (int64_t)rank * kThreads + tid; i < (int64_t)tile.count * P.n; i += kCluster * kThreads) {
-            const int64_t r = i / P.n, c = i % P.n;
-            out[r * P.out_stride + c] = y[r * P.y_stride + c];
+        const int first = (int)((int64_t)blocks_n * rank / C) * 32, last = min((int)((int64_t)blocks_n * (rank + 1) / C) * 32, P.n);
+        for (int r = warp; r < tile.count; r += kThreads / 32) {
+            const T *const from = y + r * P.y_stride;
+            T *const to = out + r * P.out_stride;
+#pragma unroll 4
+            for (int c = first + lane * E; c < last; c += 32 * E) {
+                if (P.vec_y && c + E <= last) *reinterpret_cast<uint4 *>(to + c) = *reinterpret_cast<const uint4 *>(from + c);
+                else
+                    for (int i = c; i < min(c + E, last); ++i) to[i] = from[i];
+            }
         }
         return;
     }
 
-    // ---- inner sums: x [16 rows] times A^T [RP], this block's blocks of features
-    float acc[NT][4];
+    // ---- inner sums: x [rows] times A^T [RP], this block's blocks of features
+    bool in[2];                                          // rows g and g + 8
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+    for (int i = 0; i < 2; ++i) in[i] = row0 + 8 * i + g < tile.count;
+    float acc[NT][4] = {};
     {
         const int nb = P.kp / BLOCK;
-        const int lo = nb * rank / kCluster, hi = nb * (rank + 1) / kCluster;
-        const bool in0 = row0 + g < tile.count, in1 = row0 + g + 8 < tile.count;
-        const T *const x0 = static_cast<const T *>(P.x) + (int64_t)(tile.row + (in0 ? row0 + g : 0)) * P.x_stride;
-        const T *const x1 = static_cast<const T *>(P.x) + (int64_t)(tile.row + (in1 ? row0 + g + 8 : 0)) * P.x_stride;
-        const T *const w = static_cast<const T *>(P.a) + ((int64_t)who * RP + g) * P.kp;
-        auto fetch = [&](const T *row, bool in, int at) {
-            uint4 r = make_uint4(0, 0, 0, 0);
-            if (in) {
-                if (P.vec_x && at + E <= P.k) r = __ldg(reinterpret_cast<const uint4 *>(row + at));
-                else {
-                    T v[E];
+        const int lo = nb * rank / C, hi = nb * (rank + 1) / C;
+        const T *const x = static_cast<const T *>(P.x) + (int64_t)tile.row * P.x_stride;
+        const uint4 *const w = reinterpret_cast<const uint4 *>(static_cast<const T *>(P.a) + (int64_t)who * RP * P.kp) + lane;
+        const auto part_of_row = [&](int i, int at) {    // features at .. of row i, where they are not all there or not aligned
+            const T *const row = x + (row0 + 8 * i + g) * P.x_stride;
+            T v[E];
+            uint4 all;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) v[e] = at + e < P.k ? row[at + e] : T(0.0f);
-                    memcpy(&r, v, 16);
+            for (int e = 0; e < E; ++e) v[e] = in[i] && at + e < P.k ? row[at + e] : T(0.0f);
+            memcpy(&all, v, 16);
+            return all;
+        };
+        const auto stage = [&](int b, int slot) {        // (many rows)
+            const int at = b * BLOCK + t * E;
+            uint4 *const to = ring + slot * R::SLOT;
+            if (b < hi) {
+#pragma unroll
+                for (int j = 0; j < NT; j += 4)
+                    if (j + warp % 4 < NT) copy16(smem_u32(to + (j + warp % 4) * 32), w + ((int64_t)b * NT + j + warp % 4) * 32, 16);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (in[i] && P.vec_x && at + E <= P.k) copy16(smem_u32(to + own + i * 32), x + (row0 + 8 * i + g) * P.x_stride + at, 16);
+                    else to[own + i * 32] = part_of_row(i, at);
                 }
             }
-            return r;
+            copy_commit();
         };
-#pragma unroll 2
-        for (int b = WIDE ? lo : lo + warp; b < hi; b += WIDE ? 1 : kWarps) {
+        struct { uint4 u[2], w[NT]; } now, next;
+        const auto ask = [&](int b, auto &f) {
             const int at = b * BLOCK + t * E;
-            const uint4 u0 = fetch(x0, in0, at), u1 = fetch(x1, in1, at);
 #pragma unroll
-            for (int j = 0; j < NT; ++j) mma_block<DT>(acc[j], u0, u1, __ldg(reinterpret_cast<const uint4 *>(w + (int64_t)8 * j * P.kp + at)));
+            for (int i = 0; i < 2; ++i)
+                f.u[i] = in[i] && P.vec_x && at + E <= P.k ? __ldg(reinterpret_cast<const uint4 *>(x + (row0 + 8 * i + g) * P.x_stride + at)) : part_of_row(i, at);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) f.w[j] = __ldg(w + ((int64_t)b * NT + j) * 32);
+        };
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < DEPTH - 1; ++i) stage(lo + turn + i * SHARE, i);
+            int slot = 0;
+#pragma unroll 1
+            for (int b = lo + turn; b < hi; b += SHARE) {
+                copy_wait<DEPTH - 2>();
+                group_sync(turn);                        // (this step's copies are there, nobody reads the last step's any more)
+                stage(b + (DEPTH - 1) * SHARE, slot == 0 ? DEPTH - 1 : slot - 1);
+                const uint4 *const from = ring + slot * R::SLOT;
+                const Left<DT> left(from[own], from[own + 32]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) mma_block(acc[j], left, from[j * 32]);
+                slot = slot + 1 == DEPTH ? 0 : slot + 1;
+            }
+            group_sync(turn);
+        } else {
+            int b = lo + turn;
+            if (AHEAD_IN && b < hi) ask(b, now);
+            for (; b < hi; b += SHARE) {
+                if (!AHEAD_IN) ask(b, now);
+                else if (b + SHARE < hi) ask(b + SHARE, next);
+                const Left<DT> left(now.u[0], now.u[1]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) mma_block(acc[j], left, now.w[j]);
+                if (AHEAD_IN) now = next;
+            }
         }
     }
-    {
-        float *const mine = part + warp * 16 * RP;
+    // ---- what the outer product's first blocks of channels take is asked for ahead of the meetings
+    const uint4 *const B = reinterpret_cast<const uint4 *>(static_cast<const T *>(P.b) + (int64_t)who * P.np * RP) + lane;
+    const int out_lo = (int)((int64_t)blocks_n * rank / C), out_hi = (int)((int64_t)blocks_n * (rank + 1) / C);
+    constexpr int STEPS = O::STEPS;
+    struct Channels { uint4 w[STEPS][O::LOADS], y[2][8 / E]; };
+    const auto ask = [&](int b, Channels &f) {
+        // column g of tile j is channel 8 (g/2) + 2 j + g%2 of the 32: a lane's sums are then channels 8t .. 8t + 7
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            *reinterpret_cast<float2 *>(mine + g * RP + 8 * j + 2 * t) = make_float2(acc[j][0], acc[j][1]);
-            *reinterpret_cast<float2 *>(mine + (g + 8) * RP + 8 * j + 2 * t) = make_float2(acc[j][2], acc[j][3]);
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+            for (int j = 0; j < O::LOADS; ++j) f.w[st][j] = __ldg(B + (((int64_t)b * STEPS + st) * O::LOADS + j) * 32);
+        const int c = b * 32 + 8 * t;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if (in[r] && P.vec_y && c + 8 <= P.n) {
+#pragma unroll
+                for (int i = 0; i < 8 / E; ++i) f.y[r][i] = reinterpret_cast<const uint4 *>(y + (int64_t)(row0 + g + 8 * r) * P.y_stride + c)[i];
+            }
+    };
+    const auto stage = [&](int b, int slot) {            // (many rows)
+        const int c = b * 32 + 8 * t;
+        uint4 *const to = ring + slot * R::SLOT;
+        if (b < out_hi) {
+            constexpr int LOADS = STEPS * O::LOADS;
+#pragma unroll
+            for (int j = 0; j < LOADS; j += 4)
+                if (j + warp % 4 < LOADS) copy16(smem_u32(to + (j + warp % 4) * 32), B + ((int64_t)b * LOADS + j + warp % 4) * 32, 16);
+            if (P.vec_y && c + 8 <= P.n) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8 / E; ++i)
+                        if (in[r]) copy16(smem_u32(to + own + (r * (8 / E) + i) * 32), y + (int64_t)(row0 + g + 8 * r) * P.y_stride + c + i * E, 16);
+            }
         }
+        copy_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < (WIDE ? DEPTH - 1 : 0); ++i) stage(out_lo + turn + i * SHARE, i);
+    Channels ahead;
+    if (AHEAD_OUT && out_lo + turn < out_hi) ask(out_lo + turn, ahead);
+    // ---- the shares of the warps with the same rows: side by side (16 rows), or each added to those before it
+#pragma unroll
+    for (int w = 0; w < (WIDE ? SHARE : 1); ++w) {
+        if (!WIDE || turn == w) {
+            float *const mine = part + (WIDE ? row0 : warp * 16) * RP;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    float2 &at = *reinterpret_cast<float2 *>(mine + (8 * i + g) * RP + 8 * j + 2 * t);
+                    float2 v = make_float2(acc[j][2 * i], acc[j][2 * i + 1]);
+                    if (w > 0) v = make_float2(at.x + v.x, at.y + v.y);
+                    at = v;
+                }
+        }
+        __syncthreads();
     }
-    __syncthreads();
+    const auto keep = [&](int i, float4 v) {             // sums i .. i + 3 of all: a rank's padding times an infinity is no 0
+        const int at = i % RP;
+        return make_float4(at < P.rank ? v.x : 0.0f, at + 1 < P.rank ? v.y : 0.0f, at + 2 < P.rank ? v.z : 0.0f, at + 3 < P.rank ? v.w : 0.0f);
+    };
+    const auto four = [](float *p) -> float4 & { return *reinterpret_cast<float4 *>(p); };
     if (!WIDE) {                                         // the four warps' shares, into the first one's place
-        for (int i = tid; i < 16 * RP; i += kThreads) part[i] = (part[i] + part[16 * RP + i]) + (part[32 * RP + i] + part[48 * RP + i]);
+        for (int i = 4 * tid; i < 16 * RP; i += 4 * kThreads) four(part + i) = (four(part + i) + four(part + 16 * RP + i)) + (four(part + 32 * RP + i) + four(part + 48 * RP + i));
     }
     cluster_arrive();
     cluster_wait();
     // ---- the cluster's shares, into this block's own memory: the sums of all eight
-    if (WIDE) {                                          // each block adds up an eighth, then all fetch the eighths
-        constexpr int EIGHTH = 64 * RP / kCluster;
-        for (int i = tid; i < EIGHTH; i += kThreads) {
-            float v = 0.0f;
+    const auto all = [&](int i) {
+        float4 v[kCluster] = {};
 #pragma unroll
-            for (int c = 0; c < kCluster; ++c) v += far_load(part + rank * EIGHTH + i, c);
-            total[i] = (rank * EIGHTH + i) % RP < P.rank ? v : 0.0f;      // (padding times an infinity is no 0)
-        }
+        for (int c = 0; c < kCluster; ++c)
+            if (c < C) v[c] = far_load(part + i, c);
+        return keep(i, ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+    };
+    // (nobody's memory goes before all have read it: waited for at the end)
+    if (WIDE) {                                          // each block adds up its part of the sums, in place: nobody else reads that part here
+        const int size = 64 * RP / C;
+        for (int i = 4 * tid; i < size; i += 4 * kThreads) four(part + rank * size + i) = all(rank * size + i);
         cluster_arrive();
         cluster_wait();
-        for (int i = tid; i < 64 * RP; i += kThreads) part[i] = far_load(total + i % EIGHTH, i / EIGHTH);
-        __syncthreads();
-    } else {
-        float *const sums = part + 16 * RP;              // (a place that nobody reads from afar)
-        for (int i = tid; i < 16 * RP; i += kThreads) {
-            float v = 0.0f;
 #pragma unroll
-            for (int c = 0; c < kCluster; ++c) v += far_load(part + i, c);
-            sums[i] = i % RP < P.rank ? v : 0.0f;
-        }
-        __syncthreads();
+        for (int i = 4 * tid; i < 64 * RP; i += 4 * kThreads)
+            if (i / size != rank) four(part + i) = far_load(part + i, i / size);
+    } else {                                             // (into a place that nobody reads from afar)
+        for (int i = 4 * tid; i < 16 * RP; i += 4 * kThreads) four(part + 16 * RP + i) = all(i);
     }
-    cluster_arrive();                                    // (nobody's memory goes before all have read it: waited for at the end)
+    __syncthreads();
+    cluster_arrive();
     const float *const h = WIDE ? part : part + 16 * RP;
 
     // ---- each row's power of two (fp16), with the adapter's scale
@@ -239,72 +411,83 @@ template <int DT, int RP, int ROWS> __global__ void __launch_bounds__(kThreads) 
     const float s = P.scale[who];
 
     // ---- outer product: h [16 rows][RP] times B^T, 32 channels at a time
-    const bool in0 = row0 + g < tile.count, in1 = row0 + g + 8 < tile.count;
-    const float f0 = row_scale[row0 + g], f1 = row_scale[row0 + g + 8];
-    const float *const h0 = h + (row0 + g) * RP, *const h1 = h + (row0 + g + 8) * RP;
-    constexpr int STEPS = RP / BLOCK > 0 ? RP / BLOCK : 1;       // 16 bytes of a row of B at a time (8 where the rank is 16 in fp16)
-    constexpr bool HALF = RP < BLOCK;
-    uint4 u0[DT == XGEN_F32 ? 1 : STEPS], u1[DT == XGEN_F32 ? 1 : STEPS];
-    if constexpr (DT != XGEN_F32) {
-        constexpr int W = HALF ? 4 : 8;
+    constexpr int W = HALF ? 4 : E;                      // a lane's inner sums of a row at a time
+    float by[2];
+    uint4 u[2][STEPS];                               // (fp16)
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-            uint32_t p[2][4] = {};
+    for (int i = 0; i < 2; ++i) {
+        const int row = row0 + 8 * i + g;
+        const float f = row_scale[row];
+        by[i] = s / f;
+        if constexpr (DT != XGEN_F32) {
 #pragma unroll
-            for (int e = 0; e < W / 2; ++e) {
-                const int at = st * BLOCK + t * W + 2 * e;
-                const __half2 v0 = __floats2half2_rn(h0[at] * f0, h0[at + 1] * f0), v1 = __floats2half2_rn(h1[at] * f1, h1[at + 1] * f1);
-                memcpy(&p[0][e], &v0, 4);
-                memcpy(&p[1][e], &v1, 4);
+            for (int st = 0; st < STEPS; ++st) {
+                uint32_t p[4] = {};
+#pragma unroll
+                for (int e = 0; e < W / 2; ++e) {
+                    const float2 two = *reinterpret_cast<const float2 *>(h + row * RP + st * BLOCK + t * W + 2 * e);
+                    const __half2 v = __floats2half2_rn(two.x * f, two.y * f);
+                    memcpy(&p[e], &v, 4);
+                }
+                u[i][st] = make_uint4(p[0], p[1], p[2], p[3]);
             }
-            u0[st] = make_uint4(p[0][0], p[0][1], p[0][2], p[0][3]);
-            u1[st] = make_uint4(p[1][0], p[1][1], p[1][2], p[1][3]);
         }
     }
-    const T *const B = static_cast<const T *>(P.b) + (int64_t)who * P.np * RP;
-    const float s0 = s / f0, s1 = s / f1;
-    const int lo = (int)((int64_t)blocks_n * rank / kCluster), hi = (int)((int64_t)blocks_n * (rank + 1) / kCluster);
-    for (int b = WIDE ? lo : lo + warp; b < hi; b += WIDE ? 1 : kWarps) {
+    int slot = 0;
+#pragma unroll 1
+    for (int b = out_lo + turn; b < out_hi; b += SHARE) {
+        Channels now;
+        const uint4 *const from_ring = ring + slot * R::SLOT;
+        if (WIDE) {
+            copy_wait<DEPTH - 2>();
+            group_sync(turn);
+            stage(b + (DEPTH - 1) * SHARE, slot == 0 ? DEPTH - 1 : slot - 1);
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
+        } else if (AHEAD_OUT) {
+            now = ahead;
+            if (b + SHARE < out_hi) ask(b + SHARE, ahead);
+        } else ask(b, now);
+        const auto w = [&](int st, int j) { return WIDE ? from_ring[(st * O::LOADS + j) * 32] : now.w[st][j]; };
+        const int c = b * 32 + 8 * t;
         float d[4][4] = {};
-        // column g of tile j is channel 8 (g/2) + 2 j + g%2 of the 32: a lane's sums are then channels 8t .. 8t + 7
-        const T *const w = B + (int64_t)(b * 32 + 8 * (g >> 1) + (g & 1)) * RP;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
+            if constexpr (HALF) {
+                const uint32_t a[4] = {u[0][0].x, u[1][0].x, u[0][0].y, u[1][0].y};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (DT == XGEN_F32) {
-                    const uint4 v0 = *reinterpret_cast<const uint4 *>(h0 + st * BLOCK + t * E), v1 = *reinterpret_cast<const uint4 *>(h1 + st * BLOCK + t * E);
-                    mma_block<DT>(d[j], v0, v1, __ldg(reinterpret_cast<const uint4 *>(w + 2 * j * RP + st * BLOCK + t * E)));
-                } else if constexpr (HALF) {
-                    const uint2 v = __ldg(reinterpret_cast<const uint2 *>(w + 2 * j * RP + t * 4));
-                    const uint32_t a[4] = {u0[0].x, u1[0].x, u0[0].y, u1[0].y};
-                    mma16(d[j], a, v.x, v.y);
-                } else mma_block<DT>(d[j], u0[st], u1[st], __ldg(reinterpret_cast<const uint4 *>(w + 2 * j * RP + st * BLOCK + t * E)));
+                for (int j = 0; j < 2; ++j) {
+                    const uint4 v = w(0, j);
+                    mma16(d[2 * j], a, v.x, v.y);
+                    mma16(d[2 * j + 1], a, v.z, v.w);
+                }
+            } else {
+                const auto of = [&](int i) { return DT == XGEN_F32 ? *reinterpret_cast<const uint4 *>(h + (row0 + 8 * i + g) * RP + st * BLOCK + t * E) : u[i][st]; };
+                const Left<DT> left(of(0), of(1));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) mma_block(d[j], left, w(st, j));
             }
         }
-        const int c = b * 32 + 8 * t;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            if (!(r ? in1 : in0) || c >= P.n) continue;
+            if (!in[r] || c >= P.n) continue;
             const int row = row0 + g + 8 * r;
             const T *const from = y + (int64_t)row * P.y_stride + c;
             T *const to = out + (int64_t)row * P.out_stride + c;
-            const float by = r ? s1 : s0;
+            const float f = by[r];
             if (P.vec_y && c + 8 <= P.n) {
                 T v[8];
                 uint4 raw[8 / E];
 #pragma unroll
-                for (int i = 0; i < 8 / E; ++i) raw[i] = reinterpret_cast<const uint4 *>(from)[i];
-                memcpy(v, raw, sizeof v);
+                for (int i = 0; i < 8 / E; ++i) memcpy(v + i * E, WIDE ? from_ring + own + (r * (8 / E) + i) * 32 : &now.y[r][i], 16);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = narrow<T>(fmaf(by, d[i >> 1][2 * r + (i & 1)], widen(v[i])));
+                for (int i = 0; i < 8; ++i) v[i] = narrow<T>(fmaf(f, d[i >> 1][2 * r + (i & 1)], widen(v[i])));
                 memcpy(raw, v, sizeof v);
 #pragma unroll
                 for (int i = 0; i < 8 / E; ++i) reinterpret_cast<uint4 *>(to)[i] = raw[i];
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (c + i < P.n) to[i] = narrow<T>(fmaf(by, d[i >> 1][2 * r + (i & 1)], widen(from[i])));
+                    if (c + i < P.n) to[i] = narrow<T>(fmaf(f, d[i >> 1][2 * r + (i & 1)], widen(from[i])));
             }
         }
     }
@@ -312,14 +495,16 @@ template <int DT, int RP, int ROWS> __global__ void __launch_bounds__(kThreads) 
     cluster_wait();
 }
 
-template <int DT> static const void *kernel(int rp, bool wide) {
-    switch (rp) {
-    case 16: return wide ? (const void *)adapters_kernel<DT, 16, 64> : (const void *)adapters_kernel<DT, 16, 16>;
-    case 32: return wide ? (const void *)adapters_kernel<DT, 32, 64> : (const void *)adapters_kernel<DT, 32, 16>;
-    case 64: return wide ? (const void *)adapters_kernel<DT, 64, 64> : (const void *)adapters_kernel<DT, 64, 16>;
-    default: return wide ? (const void *)adapters_kernel<DT, 128, 64> : (const void *)adapters_kernel<DT, 128, 16>;
-    }
+constexpr int kSharedMost = 227 << 10;                   // of a block, with what the system keeps
+constexpr int static_bytes(int rp) { return 256 * rp + 512; }
+struct Kernel { const void *run; int shared; };
+template <int DT, int RP> static Kernel kernel(bool wide) {
+    return wide ? Kernel{(const void *)adapters_kernel<DT, RP, 64>, Ring<DT, RP>::BYTES} : Kernel{(const void *)adapters_kernel<DT, RP, 16>, 0};
 }
+template <int DT> static Kernel kernel(int rp, bool wide) {
+    return rp == 16 ? kernel<DT, 16>(wide) : rp == 32 ? kernel<DT, 32>(wide) : rp == 64 ? kernel<DT, 64>(wide) : kernel<DT, 128>(wide);
+}
+static Kernel kernel_of(int dt, int rp, bool wide) { return dt == XGEN_F32 ? kernel<XGEN_F32>(rp, wide) : kernel<XGEN_F16_F32ACC>(rp, wide); }
 
 }  // namespace adapters
 
@@ -357,26 +542,35 @@ xgen_status xgen_adapters_pack(const xgen_adapters_desc *d, const void *a, const
     alloc((void **)&h->d_scale, (size_t)d->adapters * 4);
     alloc((void **)&h->d_status, 4);
     auto good = [&](cudaError_t e) { if (st == XGEN_OK && e != cudaSuccess) st = XGEN_ERR_CUDA; };
+    for (int wide = 0; wide < 2 && st == XGEN_OK; ++wide)
+        good(cudaFuncSetAttribute(kernel_of(d->dtype, rp, wide).run, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost - 1024 - static_bytes(rp)));
     if (st == XGEN_OK) {
+        good(cudaDeviceGetAttribute(&h->processors, cudaDevAttrMultiProcessorCount, device));
         good(cudaMemset(h->d_status, 0, 4));
         good(cudaMemcpy(h->d_scale, scale, (size_t)d->adapters * 4, cudaMemcpyHostToDevice));
-        // one matrix at a time, its rows padded
-        const auto upload = [&](void *to, const void *from, int rows, int cols, int rows_p, int cols_p) {
-            const size_t one = (size_t)rows_p * cols_p * eb;
-            std::vector<char> padded;
+        // one matrix at a time, padded with zeros, in the order of struct Order; place(row, column): where an element goes
+        const auto upload = [&](void *to, const void *from, int rows, int cols, size_t elements, auto place) {
+            std::vector<char> stored;
             try {
-                padded.assign(one, 0);
+                stored.assign(elements * eb, 0);
             } catch (const std::bad_alloc &) {
                 st = XGEN_ERR_ALLOC;
             }
             for (int i = 0; i < d->adapters && st == XGEN_OK; ++i) {
+                const char *at = static_cast<const char *>(from) + (size_t)i * rows * cols * eb;
                 for (int r = 0; r < rows; ++r)
-                    std::memcpy(padded.data() + (size_t)r * cols_p * eb, static_cast<const char *>(from) + ((size_t)i * rows + r) * cols * eb, (size_t)cols * eb);
-                good(cudaMemcpy(static_cast<char *>(to) + i * one, padded.data(), one, cudaMemcpyHostToDevice));
+                    for (int c = 0; c < cols; ++c, at += eb) std::memcpy(stored.data() + place(r, c) * eb, at, eb);
+                good(cudaMemcpy(static_cast<char *>(to) + i * stored.size(), stored.data(), stored.size(), cudaMemcpyHostToDevice));
             }
         };
-        upload(h->d_a, a, d->rank, d->k, rp, kp);
-        upload(h->d_b, b, d->c_out, d->rank, np, rp);
+        const int e = (int)(16 / eb), block = 4 * e;
+        upload(h->d_a, a, d->rank, d->k, (size_t)rp * kp, [&](int r, int f) { return ((size_t)(f / block) * rp + r) * block + f % block; });
+        upload(h->d_b, b, d->c_out, d->rank, (size_t)rp * np, [&](int c, int r) {
+            const bool half = rp < block;
+            const int w = half ? 4 : e, j = c % 8 / 2, g = c % 32 / 8 * 2 + c % 2, lane = 4 * g + r / w % 4;
+            const size_t step = (size_t)(c / 32) * (half ? 1 : rp / block) + r / (4 * w);
+            return half ? ((step * 2 + j / 2) * 32 + lane) * 8 + j % 2 * 4 + r % w : ((step * 4 + j) * 32 + lane) * e + r % w;
+        });
         good(cudaDeviceSynchronize());
     }
     if (st != XGEN_OK) {
@@ -414,14 +608,25 @@ xgen_status xgen_adapters_run(const xgen_adapters_packed *h, const void *x, int6
     P.vec_x = (uintptr_t)x % 16 == 0 && x_stride * eb % 16 == 0;
     P.vec_y = ((uintptr_t)y | (uintptr_t)out) % 16 == 0 && y_stride * eb % 16 == 0 && out_stride * eb % 16 == 0;
     P.in_place = in_place;
-    const bool wide = rows / requests >= 32;
+    // (64 requests, rank 16, of 64 rows on average: 52 us by the kernel for many rows, 40 by the other; of 96 66 and 71 us; 8 requests of
+    // 64 rows 13.4 and 9.5 us, of 96 14.2 and 12.0)
+    const bool wide = rows / requests >= 64;
     const int64_t tiles = rows / (wide ? 64 : 16) + (requests < rows ? requests : rows);
     if (tiles > INT32_MAX / kCluster) return XGEN_ERR_SHAPE;
+    // Clusters as large as all of them fit on the device at once: a few that come after the others take as long as those.
+    // (Clusters of 8, 4, 2: 77 of many rows at rank 64 53, 46, 59 us, 317 of them 197, 162, 138 us; 200 single rows at rank 64 56,
+    // 38, 32 us, 48 at rank 16 9.2, 10.2, 15.0 us.  At 1000 rows single blocks are 6 % faster still.)
+    P.cluster = kCluster;
+    while (P.cluster > 2 && tiles * P.cluster > h->processors * resident(h->d.dtype, h->rp, wide)) P.cluster /= 2;
+    const Kernel k = kernel_of(h->d.dtype, h->rp, wide);
+    // The device puts clusters side by side on an SM while others stay empty: memory that nobody uses keeps them apart.  (48 rows of 48
+    // requests 11.0 us without, 9.2 with it; 4600 rows at rank 32 43.8 and 36.3 us.)  17/20: not every SM can be in a cluster.
+    const int64_t need = (tiles * P.cluster * 20 + h->processors * 17 - 1) / (h->processors * 17);
+    const int shared = max(k.shared, (int)(kSharedMost / need) - 1024 - static_bytes(h->rp));
     OnDevice on(h->device);
     if (!on.ok) return XGEN_ERR_CUDA;
     void *args[] = {&P};
-    return launch(h->d.dtype == XGEN_F32 ? kernel<XGEN_F32>(h->rp, wide) : kernel<XGEN_F16_F32ACC>(h->rp, wide), dim3((unsigned)(tiles * kCluster)),
-                  dim3(kThreads), 0, stream, args, kCluster);
+    return launch(k.run, dim3((unsigned)(tiles * P.cluster)), dim3(wide ? 256 : 128), shared, stream, args, P.cluster);
 }
 
 xgen_status xgen_adapters_last_status(const xgen_adapters_packed *h, void *stream) {

@@ -72,6 +72,22 @@ def test_strides_and_alignment(dtype, strides, shift, n):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("strides,shift", [((136, 104, 104), 0), ((137, 101, 103), 1)])
+@pytest.mark.parametrize("n", [[1, 3, 1, 16], [90, 70, 130, 64]])
+def test_rows_of_no_adapter(dtype, strides, shift, n):
+    """Copied as they are, a bit pattern for a bit pattern, whatever the alignment."""
+    check(dtype, n, [-1, 0, -1, -1], 136, 100, 16, strides=strides, shift=shift)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("rank", [16, 64, 128])
+@pytest.mark.parametrize("n", [[1] * 180, [1, 2] * 300, [70] * 70, [64, 65] * 120])
+def test_many_requests(dtype, rank, n):
+    """More tiles than the device holds as clusters of eight: they become clusters of four, of two."""
+    check(dtype, n, [i % 5 - 1 for i in range(len(n))], 200, 104, rank, count=4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
 def test_infinities_and_nan_stay_in_their_rows(dtype):
     """A row of x with a NaN is lost, its neighbours are not; rows of no adapter and result rows keep what they hold."""
     def edit(x, y):
