@@ -31,8 +31,9 @@
  * Attention: query head h uses key/value head h / (q_heads/kv_heads).  The row at position p sees the tokens j <= p,
  * with a window only j > p - window.
  *   y = sum_j softmax_j( softmax_scale * <turned q, k_j> ) v_j
- * A row that sees nothing gives zeros.  Scores, maxima and sums are fp32.  fp16 layers round turned queries and
- * probabilities to 11 bits; fp32 layers keep 22.
+ * A row that sees nothing gives zeros.  Maxima and sums are fp32.  A turned query row becomes integers of 16 bits (fp32
+ * layers: 24) times its largest magnitude / 32512 (8323072); their products with the codes are exact.  Probabilities have 11 bits (fp32 layers:
+ * 22), relative to the largest of their row so far.
  *
  * Pages outside 0 .. pages-1 (or beyond table_stride) are not touched: appending to one is left out, its
  * tokens are seen by nobody and read as zeros, and xgen_attention_last_status reports it.  A page that is appended to belongs to one
@@ -109,7 +110,7 @@ xgen_status xgen_attention_read(const xgen_attention_packed *packed, const xgen_
                                 xgen_dtype out_dtype, void *k_out_dev, void *v_out_dev, int64_t out_stride, void *cuda_stream);
 
 /* Bytes of workspace that xgen_attention_run takes for this batch's sequences, rows and longest (the device pointers
- * are not looked at).  It grows with each of them.  Errors: INVALID_ARG, SHAPE, CUDA (host-only handle). */
+ * are not looked at).  It grows with rows and longest, so what does for a batch does for every smaller one.  Errors: INVALID_ARG, SHAPE, CUDA (host-only handle). */
 xgen_status xgen_attention_workspace(const xgen_attention_packed *packed, const xgen_attention_batch *batch, int64_t *bytes);
 
 /*
@@ -118,13 +119,15 @@ xgen_status xgen_attention_workspace(const xgen_attention_packed *packed, const 
  *   y_dev  [rows] rows likewise, y_stride apart, outside q_dev
  *   workspace_dev  xgen_attention_workspace bytes, 16-byte aligned.  Nothing in it counts between calls; calls that
  *          may run at the same time need one each
- * Only enqueues kernels.  Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (rows times q_heads / kv_heads above 2^31 too), CUDA.
+ * Only enqueues kernels: two for a few rows of each sequence, three more where a sequence may have many.
+ * Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (rows times q_heads / kv_heads above 2^31 too), CUDA.
  */
 xgen_status xgen_attention_run(const xgen_attention_packed *packed, const void *q_dev, int64_t q_stride, const xgen_attention_batch *batch,
                                const xgen_attention_cache *cache, void *y_dev, int64_t y_stride, void *workspace_dev, void *cuda_stream);
 
 /* Synchronise the stream and report the first error seen: XGEN_OK, XGEN_ERR_CUDA, or, once, XGEN_ERR_INVALID_ARG
- * after a call that met a page that is not there or a sequence longer than it said. */
+ * after a call that met a page that is not there or a sequence longer than it said, or XGEN_ERR_TIMEOUT after one in which
+ * a kernel's own waits ran out (two seconds; its results are not complete). */
 xgen_status xgen_attention_last_status(const xgen_attention_packed *packed, void *cuda_stream);
 
 /* Release the handle and its device memory.  NULL is allowed. */

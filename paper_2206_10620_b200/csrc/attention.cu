@@ -4,11 +4,11 @@
 //         (turned there, if keys) until their largest magnitude has decided the page's scale.  A token's angle is that of the page's first token, worked
 //         out once for each of a thread's pairs, and that of its slot, from a table made with the handle.
 // read    codes times scales; blocks as for append, 16 bytes of the result a thread at a time.
-// run     `narrow_kernel`: few query rows (up to 16 with all query heads of a key head) against the whole cache of a sequence, bound
+// run     `narrow_kernel`: few query rows (with all query heads of a key head) against the whole cache of a sequence, bound
 //         by the cache's bytes.  The work of a call is a line of units (64 tokens of one key head, for one tile of rows), cut into
 //         equal pieces, one for each block that the GPU holds at once; where a cut falls inside a tile's tokens the pieces
 //         leave partial results, which `combine_kernel` joins in their order.  So any mixture of lengths fills the GPU evenly.
-//
+//         Sequences of many rows are wide_kernel's, in attention_wide.cu, cut and joined the same way.
 // Scores are exact integer products: a query row is a factor times integers of 16 bits (fp32: 24), split into two (three) signed
 // bytes, and integer matrix instructions multiply each with the key codes as they lie in the cache.  Values meet probabilities
 // in fp16 (fp32: in two parts): a code is exact there, widened by byte permutes and one subtraction.  The page's scales are
@@ -1016,13 +1016,15 @@ struct Route {
     int eights;                 // narrow_kernel's tiles, in eights of rows; 0: not launched
     bool wide;
 };
-// Up to 16 rows of every sequence (with all query heads of a key head) are narrow_kernel's, in tiles of eight where that holds them.  Where there
-// may be more, wide_kernel takes the sequences that have more, and narrow_kernel is launched too unless all must have.
-// us at 16 and 32 rows of 8 sequences over 8192 tokens: see the comment at kNarrowMost's use in DESIGN's table of cases.
+// Few rows of every sequence (with all query heads of a key head) are narrow_kernel's, in tiles of eight where that holds them, else in tiles of
+// 16.  Where a sequence may have more, wide_kernel takes those that have more than 16, and narrow_kernel is launched too unless
+// all must have.  us by narrow_kernel and by wide_kernel, four query heads to a key head, dim 128, fp16: up to 32 rows of 8
+// sequences over 8192 tokens 51 and 109, of 64 over 2000 105 and 134; up to 64 rows 77 and 89, 178 and 151, of 8 over 1024 28 and
+// 44.  (Both, each with some of the sequences, are slower than either there: 115, 166, 61.)
 static Route route_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
     const int64_t group = h.d.q_heads / h.d.kv_heads, most = (int64_t)b.longest * group;
     if (most <= 8) return {1, false};
-    if (most <= kNarrowMost || !h.wide_workers || b.sequences > kWideSequences) return {2, false};
+    if (most <= kNarrowAlone || !h.wide_workers || b.sequences > kWideSequences) return {2, false};
     const int64_t least = b.rows - (int64_t)(b.sequences - 1) * b.longest;       // rows of the shortest sequence, at least
     return {least * group > kNarrowMost ? 0 : 2, true};
 }
@@ -1030,11 +1032,14 @@ static int64_t part_bytes(const xgen_attention_packed &h, int64_t workers, int64
     return (workers * 2 * rows * (h.d.head_dim * 4 + 16) + workers * (int64_t)sizeof(Cut) + 255) / 256 * 256;
 }
 static int64_t narrow_bytes(const xgen_attention_packed &h, const Route &r) { return r.eights ? part_bytes(h, h.workers[r.eights - 1], 8 * r.eights) : 0; }
+// For any batch of at most these sequences, rows and rows of a sequence, whatever its route.
 static int64_t workspace_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
-    const Route r = route_of(h, b);
-    if (!r.wide) return narrow_bytes(h, r);
+    const int64_t most = (int64_t)b.longest * (h.d.q_heads / h.d.kv_heads), one = narrow_bytes(h, {1, false}), two = narrow_bytes(h, {2, false});
+    if (most <= 8) return one;
+    const int64_t narrow = one > two ? one : two;
+    if (most <= kNarrowAlone || !h.wide_workers) return narrow;
     const int64_t rows = b.rows * h.d.q_heads, terms = wide_kernel_for(h.d.dtype, h.d.head_dim).terms;
-    return narrow_bytes(h, r) + part_bytes(h, h.wide_workers, kWideRows) + (rows * terms * h.d.head_dim + rows * 4 + 255) / 256 * 256;
+    return narrow + part_bytes(h, h.wide_workers, kWideRows) + (rows * terms * h.d.head_dim + rows * 4 + 255) / 256 * 256;
 }
 
 }  // namespace attention

@@ -156,7 +156,7 @@ struct RunParams {
 
 
 // Rows of a sequence (with all query heads of a key head) up to which narrow_kernel takes it where both kernels are launched.
-constexpr int kNarrowMost = 16;
+constexpr int kNarrowMost = 16, kNarrowAlone = 64;      // beside wide_kernel; where there is none
 // The kernel for many rows (attention_wide.cu): what one needs to launch it; no kernel where the block's memory would not do.
 constexpr int kWideRows = 128, kWideThreads = kWideRows + 32, kWideUnit = 64, kWideSequences = 1024;
 struct WideKernel {

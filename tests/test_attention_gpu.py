@@ -492,3 +492,131 @@ def test_offsets_past_32_bits():
     su.close(y.t, want, bound)
     k, v = read(op, p, [300], "f16")
     su.close(k, p.values(0, 0, 300), 2.0 ** -11 * p.values(0, 0, 300).abs() + 2.0 ** -25)
+
+
+# --- many rows -------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 192, 256])
+@pytest.mark.parametrize("page", [16, 64, 128])
+def test_prompts_beside_decoding(dtype, D, page):
+    """Sequences of one row, of a few and of many in one call, over caches that end inside a page and a unit."""
+    check(dtype, [1, 700, 150, 333, 40, 64, 90], [1, 1, 150, 40, 40, 3, 17], 2, 4, D, page, seed=D + page)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("G,n", [(1, [64]), (1, [65]), (1, [127]), (1, [128]), (1, [129]), (1, [257, 1]), (3, [43]), (5, [26, 13]),
+                                 (16, [5, 9]), (32, [3, 2]), (64, [2])])
+def test_tiles_that_rows_just_fill(dtype, G, n):
+    check(dtype, [x + 70 for x in n], n, 1, G, 64, 32, seed=G)
+
+
+@pytest.mark.parametrize("window", [1, 3, 63, 64, 65, 200])
+def test_windows_of_chunks(window):
+    check("f16", [1000, 333], [300, 90], 2, 4, 128, 64, window=window, seed=window)
+    check("f32", [1000, 333], [300, 90], 1, 4, 64, 16, window=window, seed=window)
+
+
+@pytest.mark.parametrize("sequences", [1023, 1024, 1025])
+def test_more_sequences_than_one_kernel_sorts(sequences):
+    n = [1] * sequences
+    n[5], n[-1] = 40, 17
+    check("f16", [x + (7 * i) % 30 for i, x in enumerate(n)], n, 1, 4, 32, 16, longest=40)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("strides", [(1024, 0), (1032, 0), (1025, 1), (1027, 3)])
+def test_strides_of_chunks(dtype, strides):
+    check(dtype, [100, 240, 7], [90, 70, 0], 2, 8, 64, 16, strides=strides, spare=3)
+
+
+def test_chunks_with_more_rows_than_positions():
+    y = check("f16", [30, 0, 200], [60, 70, 65], 1, 2, 64, 16)
+    assert (y[:30] == 0).all() and (y[60:130] == 0).all() and (y[30:60] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_chunks_with_lost_pages(dtype):
+    """Pages that are not there are seen by nobody, a page's lost scale by those who see it, and stale pages may hold anything."""
+    H, G, D, page = 2, 4, 64, 16
+    op, freq = make(H, D, page, dtype, q_heads=H * G)
+    lengths, n = [200, 90], [100, 40]
+    for what in ("there", "k", "v"):
+        pages = su.Pages(lengths, H, D, page, seed=3)
+        spare = torch.ones(pages.pages, dtype=torch.bool, device="cuda")
+        spare[pages.table[pages.table >= 0].long()] = False
+        pages.scale[0][spare] = math.nan
+        pages.scale[1][spare] = math.inf
+        q = torch.randn((sum(n), H * G * D), device="cuda", generator=su.gen(4)).to(su.T[dtype])
+        bad = torch.zeros((sum(n), H * G), dtype=torch.bool, device="cuda")
+        if what == "there":
+            pages.table[0, 2] = pages.pages
+            pages.table[0, 9] = -1
+            pages.table[1, 5] = -7
+        else:
+            w = "kv".index(what)
+            lost = int(pages.table[0, 8])                    # tokens 128 .. 143 of sequence 0, whose rows are at 100 .. 199
+            keep = float(pages.scale[w][lost, 1])
+            pages.scale[w][lost, 1] = math.nan
+            q[110, 3] = math.nan
+            q[120, 5 * D + 1] = math.inf
+            bad[28:100, G:] = True
+            bad[110, 0] = True
+            bad[120, 5] = True
+        y = su.attend(op, pages, n, q, H * G, dtype).t.view(sum(n), H * G, D)
+        assert torch.equal(torch.isnan(y).all(2), bad) and torch.equal(torch.isnan(y).any(2), bad)
+        if what == "there":
+            with pytest.raises(binding.PatconvError) as e:
+                op.sync(su.stream())
+            assert e.value.status == 1
+        else:
+            pages.scale[w][lost, 1] = keep
+        op.sync(su.stream())
+        want, bound = su.attention(pages, n, q.nan_to_num(0, 0, 0), H * G, dtype, freq)
+        ok = ~bad.repeat_interleave(D, 1)
+        su.close(torch.where(ok, y.flatten(1).double(), 0.0), torch.where(ok, want, 0.0), bound)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_chunks_captured_and_on_two_streams(dtype):
+    """Two graphs, each with its own workspace, replayed side by side with other rows and lengths than they were captured with."""
+    H, G, D, page = 2, 4, 64, 16
+    op, freq = make(H, D, page, dtype, q_heads=H * G)
+    jobs = []
+    for seed in range(2):
+        pages = su.Pages([900, 500, 300], H, D, page, seed=seed)
+        q = torch.randn((200, H * G * D), device="cuda", generator=su.gen(seed)).to(su.T[dtype])
+        y = torch.zeros_like(q)
+        batch = pages.batch([100, 1, 60], rows=200, longest=190)
+        work = torch.full((op.workspace(batch) // 4 + 1,), float("nan"), device="cuda")
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            op.run(q.data_ptr(), H * G * D, batch, pages.handle, y.data_ptr(), H * G * D, work.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        jobs.append((pages, q, y, batch, work, stream, graph))
+    for n, lengths in [([100, 1, 60], [900, 500, 300]), ([5, 190, 0], [9, 500, 300]), ([1, 1, 180], [900, 1, 200]), ([0, 0, 0], [0, 0, 0])]:
+        for (pages, q, y, batch, work, stream, graph) in jobs:
+            pages.lengths = lengths
+            pages.length.copy_(su.ints(lengths))
+            pages._starts[-1].copy_(su.starts(n))
+            y.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for (pages, q, y, batch, work, stream, graph) in jobs:
+                with torch.cuda.stream(stream):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for (pages, q, y, batch, work, stream, graph) in jobs:
+            want, bound = su.attention(pages, n, q, H * G, dtype, freq)
+            su.close(y[:sum(n)], want, bound)
+            assert (y[sum(n):] == 7.0).all()
+    op.sync(su.stream())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_workspace_does_for_smaller_batches(dtype):
+    op, _ = make(2, 64, 16, dtype, q_heads=8)
+    def size(sequences, rows, longest):
+        return op.workspace(binding.Batch(sequences, rows, longest, 256, 256, 256, 4))
+    sizes = [size(s, r, l) for s in (1, 2, 1024, 1025) for r, l in ((1, 1), (3, 2), (40, 5), (40, 16), (40, 17), (200, 17), (200, 190))]
+    per = len(sizes) // 4
+    assert all(sizes[i] <= sizes[i + 1] for i in range(len(sizes) - 1) if (i + 1) % per)
+    assert all(sizes[i] <= sizes[i + per] for i in range(len(sizes) - per))
