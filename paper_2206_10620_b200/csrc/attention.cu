@@ -1032,6 +1032,9 @@ static int64_t part_bytes(const xgen_attention_packed &h, int64_t workers, int64
     return (workers * 2 * rows * (h.d.head_dim * 4 + 16) + workers * (int64_t)sizeof(Cut) + 255) / 256 * 256;
 }
 static int64_t narrow_bytes(const xgen_attention_packed &h, const Route &r) { return r.eights ? part_bytes(h, h.workers[r.eights - 1], 8 * r.eights) : 0; }
+static int64_t fold_bytes(const xgen_attention_packed &h) {
+    return wide_kernel_for(h.d.dtype, h.d.head_dim).folds ? (int64_t)h.wide_workers * kWideRows * h.d.head_dim * 4 : 0;
+}
 // For any batch of at most these sequences, rows and rows of a sequence, whatever its route.
 static int64_t workspace_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
     const int64_t most = (int64_t)b.longest * (h.d.q_heads / h.d.kv_heads), one = narrow_bytes(h, {1, false}), two = narrow_bytes(h, {2, false});
@@ -1039,7 +1042,7 @@ static int64_t workspace_of(const xgen_attention_packed &h, const xgen_attention
     const int64_t narrow = one > two ? one : two;
     if (most <= kNarrowAlone || !h.wide_workers) return narrow;
     const int64_t rows = b.rows * h.d.q_heads, terms = wide_kernel_for(h.d.dtype, h.d.head_dim).terms;
-    return narrow + part_bytes(h, h.wide_workers, kWideRows) + (rows * terms * h.d.head_dim + rows * 4 + 255) / 256 * 256;
+    return narrow + part_bytes(h, h.wide_workers, kWideRows) + fold_bytes(h) + (rows * terms * h.d.head_dim + rows * 4 + 255) / 256 * 256;
 }
 
 }  // namespace attention
@@ -1235,7 +1238,9 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     if (route.eights) st = attend(k.narrow, k.combine, h->workers[route.eights - 1], k.rows, kThreads, k.shared, work);
     if (st == XGEN_OK && route.wide) {
         const WideKernel w = wide_kernel_for(h->d.dtype, h->d.head_dim);
-        P.q_bytes = reinterpret_cast<int8_t *>(work + narrow_bytes(*h, route) + part_bytes(*h, h->wide_workers, kWideRows));
+        char *const behind = work + narrow_bytes(*h, route) + part_bytes(*h, h->wide_workers, kWideRows);
+        P.fold = reinterpret_cast<float4 *>(behind);
+        P.q_bytes = reinterpret_cast<int8_t *>(behind + fold_bytes(*h));
         P.q_factor = reinterpret_cast<float *>(P.q_bytes + b->rows * h->d.q_heads * (int64_t)w.terms * h->d.head_dim);
         const int64_t warps = b->rows * ((h->d.q_heads + kQueryHeads - 1) / kQueryHeads);
         void *args[] = {&P};

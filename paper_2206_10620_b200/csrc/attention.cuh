@@ -149,6 +149,7 @@ struct RunParams {
     struct Cut *cut;                 // [workers]
     int8_t *q_bytes;                 // wide_kernel: [kv_heads][rows * group][terms][dim]: the queries' integers, bytes of the lowest value first
     float *q_factor;                 // [kv_heads][rows * group]: what they are multiples of, times the scale
+    float4 *fold;                    // wide_kernel, fp32: [workers][dim/4][128 rows], where a worker keeps totals that tensor memory has no room for
     int workers, early;
     int launched;                    // how many kernels share the sequences: 1 (this one takes all) or 2
     int *status;
@@ -162,6 +163,7 @@ constexpr int kWideRows = 128, kWideThreads = kWideRows + 32, kWideUnit = 64, kW
 struct WideKernel {
     const void *kernel, *queries;    // `queries` goes before it
     int shared, blocks, terms;       // blocks: resident on an SM at once
+    bool folds;                      // it takes RunParams::fold
 };
 constexpr int kQueryThreads = 256, kQueryHeads = 4;      // a warp of `queries` takes a row's kQueryHeads heads
 WideKernel wide_kernel_for(xgen_dtype t, int dim);

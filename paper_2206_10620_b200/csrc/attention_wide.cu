@@ -49,6 +49,12 @@ template <int DT, int D> struct Wide {
     static constexpr int PROBS = kWideRows * kWideUnit * 2;
     static constexpr int SHARED = Q + 4 * CODES + VALUES + PROBS * (SPLIT ? 2 : 1);
     static constexpr int COLUMNS = TERMS * kWideUnit + D <= 256 ? 256 : 512;
+    // The matrix unit rounds sums toward zero, and each of a unit's 8 products adds to what is lost: sums over 25 units were off by
+    // 1.8e-6 on average, in one direction.  fp32 layers add up FOLD units at a time, and the totals apart: in tensor memory
+    // where there is room, else in the workspace.  Root mean square errors, and us for 2 x 1024 rows over 5000 tokens, dim 128: 2.3e-6 and
+    // 495 without, 6.9e-7 and 510 by fours, 5.1e-7 and 533 by twos; dim 64 (workspace) 1.4e-6 and 304, 7.0e-7 and 329, 5.0e-7 and 367.
+    static constexpr bool FOLD_NEAR = TERMS * kWideUnit + 2 * D <= COLUMNS;
+    static constexpr int FOLD = !SPLIT ? 1 << 30 : FOLD_NEAR ? 2 : 4;
     // Sums of two terms lose their lowest bits, so that what is left goes into 23: an error of at most what the query row's largest component
     // times 1/256 (1/128) of a key step gives (fp16 queries would have up to 16 steps' worth in a sum of 128).
     static constexpr int DROP = D <= 128 ? 7 : 8;
@@ -212,6 +218,33 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     const uint64_t q_desc = operand_desc(smem_at(qs), 128, D * 8), k_desc = operand_desc(smem_at(codes), 128, D * 8);
     const uint64_t p_desc = operand_desc(smem_at(probs), 128, kWideUnit * 16), v_desc = operand_desc(smem_at(values), D * 16, 128);
 
+    // this thread's totals, 16 at a time: (times `since`) plus r, or r alone
+    float4 *const fold = P.fold + (int64_t)worker * (D / 4) * kWideRows + tid;
+    const auto add_totals = [&](int c, uint32_t (&r)[16], float since) {
+        if constexpr (W::FOLD_NEAR) {
+            uint32_t t[16];
+            tmem_ld16(t_sums + D + my_lanes + c * 16, t);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(fmaf(__uint_as_float(t[i]), since, __uint_as_float(r[i])));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float4 t = fold[(c * 4 + i) * kWideRows];
+                const float four[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[4 * i + j] = __float_as_uint(fmaf(four[j], since, __uint_as_float(r[4 * i + j])));
+            }
+        }
+    };
+    const auto keep_totals = [&](int c, const uint32_t (&r)[16]) {
+        if constexpr (W::FOLD_NEAR) tmem_st16(t_sums + D + my_lanes + c * 16, r);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                fold[(c * 4 + i) * kWideRows] = make_float4(__uint_as_float(r[4 * i]), __uint_as_float(r[4 * i + 1]), __uint_as_float(r[4 * i + 2]), __uint_as_float(r[4 * i + 3]));
+    };
+
     bool whole = skipped == 0;
     int slot = 0;
     while (todo > 0) {
@@ -219,7 +252,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         const int row0 = tile * kWideRows, rows = min(kWideRows, q.n * G - row0), before = q.length - q.n;
         const int units = (int)min(todo, (int64_t)(w.units - skipped));
         const bool last_part = skipped + units == w.units;
-        float l = 0.0f, m = -INFINITY, unit = 0.0f;
+        float l = 0.0f, m = -INFINITY, unit = 0.0f, since = 1.0f;       // since: what the totals are to be multiplied by
         if (warp == kRowWarps) {
             // ---- codes, two steps ahead; matrix instructions, whenever the threads are done with a step (first: with the queries)
             const int token_begin = w.from + (int)skipped * kWideUnit;
@@ -283,7 +316,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
 #pragma unroll
                             for (int part = W::SPLIT ? 1 : 0; part >= 0; --part)
                                 mma_f16<false>(t_sums, (uint32_t)p_desc + part * (W::PROBS / 16) + k * 16, p_hi, (uint32_t)v_desc + k * 2 * D, v_hi, IDESC_O,
-                                               u > 0 || k > 0 || part != (W::SPLIT ? 1 : 0));
+                                               u % W::FOLD > 0 || k > 0 || part != (W::SPLIT ? 1 : 0));
                         tc_commit<false>(bar_o, 0);
                     }
                     if (u + 1 < units) {
@@ -343,6 +376,18 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         raw[i] = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
                     }
                     if (u > 0) wait(bar_o, phase_o);      // the product before: values, probabilities and sums are free
+                    if (W::SPLIT && u > 0 && u % W::FOLD == 0) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t r[16];
+                            tmem_ld16(t_sums + my_lanes + c * 16, r);
+                            tmem_wait_ld();
+                            if (u > W::FOLD) add_totals(c, r, since);
+                            keep_totals(c, r);
+                        }
+                        if (W::FOLD_NEAR) tmem_wait_st();
+                        since = 1.0f;
+                    }
 #pragma unroll
                     for (int i = 0; i < MINE; ++i) {
                         const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
@@ -455,7 +500,8 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         to[W::PROBS / 16 + 8] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
                     }
                 }
-                if (u > 0 && __any_sync(~0u, shrink != 1.0f)) {
+                since *= shrink;
+                if (u % W::FOLD > 0 && __any_sync(~0u, shrink != 1.0f)) {
 #pragma unroll 1
                     for (int c = 0; c < D / 16; ++c) {
                         uint32_t r[16];
@@ -484,6 +530,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 uint32_t r[16];
                 tmem_ld16(t_sums + my_lanes + c * 16, r);
                 tmem_wait_ld();
+                if (W::SPLIT && units > W::FOLD) add_totals(c, r, since);
                 if (tid < rows) {
                     float x[16];
 #pragma unroll
@@ -618,7 +665,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kQueryThreads) query_
 template <int DT, int D> static WideKernel wide_of() {
     using W = Wide<DT, D>;
     if constexpr (W::SHARED > 216 * 1024) return {};
-    else return {(const void *)wide_kernel<DT, D>, (const void *)query_kernel<DT, D>, W::SHARED, W::BLOCKS, W::TERMS};
+    else return {(const void *)wide_kernel<DT, D>, (const void *)query_kernel<DT, D>, W::SHARED, W::BLOCKS, W::TERMS, W::SPLIT && !W::FOLD_NEAR};
 }
 template <int DT> static WideKernel wide_dt(int dim) {
     switch (dim) {

@@ -510,6 +510,29 @@ def test_tiles_that_rows_just_fill(dtype, G, n):
     check(dtype, [x + 70 for x in n], n, 1, G, 64, 32, seed=G)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("D", [32, 64, 128, 192])
+def test_chunks_over_a_long_cache(dtype, D):
+    """So many rows that no block's piece ends within thousands of tokens; entries that differ by orders of magnitude along the cache."""
+    def edit(pages, q):
+        for w in range(2):
+            grow = 2.0 ** torch.linspace(-3, 3 - 2 * w, pages.table.shape[1], device="cuda")
+            pages.scale[w][pages.table[0].long()] *= grow[:, None]
+    check(dtype, [4500], [2200], 2, 8, D, 64, size=0.3, edit=edit, seed=D)
+
+
+def test_long_sums_are_not_short_of_their_values():
+    """fp32: sums rounded toward zero lose half a step (2^-24 at most) with every product, and no more than 16 products may
+    come before they are added up with rounding: 16 * 2^-24 of a running sum that is half of the last one on average."""
+    H, G, D, page, L, n = 1, 4, 128, 64, 5000, 1200
+    op, freq = make(H, D, page, "f32", q_heads=H * G)
+    pages = su.Pages([L], H, D, page, seed=1)
+    q = torch.randn((n, H * G * D), device="cuda", generator=su.gen(2))
+    y = su.attend(op, pages, [n], q, H * G, "f32").t.double()
+    want, _ = su.attention(pages, [n], q, H * G, "f32", freq)
+    assert abs(((y - want) * want.sign()).mean() / want.abs().mean()) < 5e-7
+
+
 @pytest.mark.parametrize("window", [1, 3, 63, 64, 65, 200])
 def test_windows_of_chunks(window):
     check("f16", [1000, 333], [300, 90], 2, 4, 128, 64, window=window, seed=window)
