@@ -87,6 +87,22 @@ def test_many_requests(dtype, rank, n):
     check(dtype, n, [i % 5 - 1 for i in range(len(n))], 200, 104, rank, count=4)
 
 
+@pytest.mark.parametrize("n", [[1] * 8, [200] * 200])
+@pytest.mark.parametrize("k", [1000, 4096])
+def test_long_sums_are_not_short_of_their_values(n, k):
+    """fp32: a matrix unit's sums are rounded toward zero, by half a step of at most 2^-23 on average.  Two of them in each of the two
+    products may lose that, the others are a thousand times smaller: 2^-22 in all, however long the sum."""
+    a, b, scale, op = make("f32", k, 256, 64, 2)
+    rows, which = sum(n), [i % 2 for i in range(len(n))]
+    x = torch.randn((rows, k), device="cuda", generator=su.gen(1))
+    y = torch.zeros((rows, 256), device="cuda")
+    want, _ = su.adapters(x, y, n, which, a, b, scale, "f32")
+    start, adapter = su.starts(n), su.ints(which)
+    op.run(x.data_ptr(), rows, k, start.data_ptr(), adapter.data_ptr(), len(n), y.data_ptr(), 256, y.data_ptr(), 256, su.stream())
+    torch.cuda.synchronize()
+    assert abs(((y - want) * want.sign()).mean() / want.abs().mean()) < 2.0 ** -22
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 def test_infinities_and_nan_stay_in_their_rows(dtype):
     """A row of x with a NaN is lost, its neighbours are not; rows of no adapter and result rows keep what they hold."""
