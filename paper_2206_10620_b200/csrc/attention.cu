@@ -752,8 +752,13 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
                         const uint32_t a[4] = {widen_codes<0x4240>(x0), widen_codes<0x4341>(x0), widen_codes<0x4240>(x1), widen_codes<0x4341>(x1)};
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            if (N::SPLIT) mma16(o[n][c + h], a, p_low[n][0], p_low[n][1]);
-                            mma16(o[n][c + h], a, p[n][0], p[n][1]);
+                            if (N::SPLIT) {                // (the matrix unit rounds sums toward zero: not the running ones of fp32 layers)
+                                float x[4] = {};
+                                mma16(x, a, p_low[n][0], p_low[n][1]);
+                                mma16(x, a, p[n][0], p[n][1]);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) o[n][c + h][i] += x[i];
+                            } else mma16(o[n][c + h], a, p[n][0], p[n][1]);
                         }
                     }
                 }

@@ -643,3 +643,14 @@ def test_workspace_does_for_smaller_batches(dtype):
     per = len(sizes) // 4
     assert all(sizes[i] <= sizes[i + 1] for i in range(len(sizes) - 1) if (i + 1) % per)
     assert all(sizes[i] <= sizes[i + per] for i in range(len(sizes) - per))
+
+
+def test_long_sums_of_single_rows_are_not_short_of_their_values():
+    """As for chunks: at most the 2 products of 16 tokens come before they are added up with rounding."""
+    H, G, D, page, L = 256, 4, 128, 64, 8000
+    op, freq = make(H, D, page, "f32", q_heads=H * G)
+    pages = su.Pages([L], H, D, page, seed=1)
+    q = torch.randn((1, H * G * D), device="cuda", generator=su.gen(2))
+    y = su.attend(op, pages, [1], q, H * G, "f32").t.double()
+    want, _ = su.attention(pages, [1], q, H * G, "f32", freq)
+    assert abs(((y - want) * want.sign()).mean() / want.abs().mean()) < 2.0 ** -23
