@@ -10,7 +10,8 @@
  *
  * and out[r] = y[r] where the request has no adapter.  Both sums are fp32; the inner one is kept to 11 bits relative to its row's
  * largest in fp16 layers, the result is rounded once.  fp32 layers keep fp32's precision throughout (relative error of
- * a sum of magnitudes about 1e-6).
+ * a sum of magnitudes about 1e-6).  A row of x, or an adapter, with values that are not finite gives results that are not
+ * finite (a NaN where the sums would be infinite, too) in the rows that use it, and in no others.
  *
  * Same conventions as patconv.h: plain C ABI, every function returns a status, *_host is host memory, *_dev
  * memory of the device the handle was packed for.

@@ -554,8 +554,9 @@ xgen_status xgen_adapters_pack(const xgen_adapters_desc *d, const void *a, const
         good(cudaDeviceGetAttribute(&h->processors, cudaDevAttrMultiProcessorCount, device));
         good(cudaMemset(h->d_status, 0, 4));
         good(cudaMemcpy(h->d_scale, scale, (size_t)d->adapters * 4, cudaMemcpyHostToDevice));
-        // one matrix at a time, padded with zeros, in the order of struct Order; place(row, column): where an element goes
-        const auto upload = [&](void *to, const void *from, int rows, int cols, size_t elements, auto place) {
+        // one matrix at a time, padded with zeros, in the order of struct Order; place(row, column): where an element goes, and
+        // those behind it up to a multiple of `run` columns
+        const auto upload = [&](void *to, const void *from, int rows, int cols, size_t elements, int run, auto place) {
             std::vector<char> stored;
             try {
                 stored.assign(elements * eb, 0);
@@ -565,13 +566,17 @@ xgen_status xgen_adapters_pack(const xgen_adapters_desc *d, const void *a, const
             for (int i = 0; i < d->adapters && st == XGEN_OK; ++i) {
                 const char *at = static_cast<const char *>(from) + (size_t)i * rows * cols * eb;
                 for (int r = 0; r < rows; ++r)
-                    for (int c = 0; c < cols; ++c, at += eb) std::memcpy(stored.data() + place(r, c) * eb, at, eb);
+                    for (int c = 0; c < cols; c += run) {
+                        const size_t n = (size_t)(cols - c < run ? cols - c : run) * eb;
+                        std::memcpy(stored.data() + place(r, c) * eb, at, n);
+                        at += n;
+                    }
                 good(cudaMemcpy(static_cast<char *>(to) + i * stored.size(), stored.data(), stored.size(), cudaMemcpyHostToDevice));
             }
         };
         const int e = (int)(16 / eb), block = 4 * e;
-        upload(h->d_a, a, d->rank, d->k, (size_t)rp * kp, [&](int r, int f) { return ((size_t)(f / block) * rp + r) * block + f % block; });
-        upload(h->d_b, b, d->c_out, d->rank, (size_t)rp * np, [&](int c, int r) {
+        upload(h->d_a, a, d->rank, d->k, (size_t)rp * kp, block, [&](int r, int f) { return ((size_t)(f / block) * rp + r) * block + f % block; });
+        upload(h->d_b, b, d->c_out, d->rank, (size_t)rp * np, rp < block ? 4 : e, [&](int c, int r) {
             const bool half = rp < block;
             const int w = half ? 4 : e, j = c % 8 / 2, g = c % 32 / 8 * 2 + c % 2, lane = 4 * g + r / w % 4;
             const size_t step = (size_t)(c / 32) * (half ? 1 : rp / block) + r / (4 * w);

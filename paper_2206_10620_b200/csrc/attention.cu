@@ -88,15 +88,15 @@ struct AppendParams {
     int *status;
 };
 
-constexpr int kAppendMost = 512;      // threads of a block: as many as it takes for kItems items each
-constexpr int kItems = 4;             // items of 8 pairs (16 components of a token) that a thread holds: 64 x 128 entries are 128 threads' work
+constexpr int kAppendMost = 512;      // threads of a block: as many as it takes for ITEMS items each
+// ITEMS: items of 8 pairs (16 components of a token) that a thread holds.
 
 // How a thread's items of a token lie: two pieces of 8 neighbours, next to each other or (a half's and the other half's) apart, or any way.
 enum Lay { PLAIN, HALVES, PAIRS, ANY };
 
 // Heads [head0, head1) of the page.  Item i of thread `tid` is pairs 8 s .. 8 s + 7 of token tid / per_token + i * (threads / per_token), s =
 // tid % per_token (the number of threads is a multiple of per_token).
-template <int DT, int LAY> __device__ __forceinline__ void append_heads(const AppendParams &P, const PagePart &part, int which, int head0, int head1) {
+template <int DT, int LAY, int ITEMS> __device__ __forceinline__ void append_heads(const AppendParams &P, const PagePart &part, int which, int head0, int head1) {
     using T = typename Elem<DT>::T;
     __shared__ unsigned most_bits[2][kAppendMost / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
@@ -112,10 +112,10 @@ template <int DT, int LAY> __device__ __forceinline__ void append_heads(const Ap
     }
     const T *const in = static_cast<const T *>(P.in[which]) + (int64_t)(part.row + token0) * P.stride;
     constexpr int W = sizeof(T) / 2;                      // 16-byte pieces of 8 components
-    uint4 raw[kItems][2 * W];
+    uint4 raw[ITEMS][2 * W];
     const auto ask = [&](int head) {
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        for (int i = 0; i < ITEMS; ++i) {
             const T *const from = in + (int64_t)(i * step) * P.stride + head * D;
             const bool there = token0 + i * step < part.n;
 #pragma unroll
@@ -128,10 +128,10 @@ template <int DT, int LAY> __device__ __forceinline__ void append_heads(const Ap
 #pragma unroll 1
     for (int head = head0; head < head1; ++head) {
         // ---- the new entries in fp32
-        float v[kItems][16];
+        float v[ITEMS][16];
         if (LAY != ANY) ask(head);
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        for (int i = 0; i < ITEMS; ++i) {
             const T *const from = in + (int64_t)(i * step) * P.stride + head * D;
             const bool there = token0 + i * step < part.n;
             if (LAY == ANY) {
@@ -148,7 +148,7 @@ template <int DT, int LAY> __device__ __forceinline__ void append_heads(const Ap
         const float was = part.slot ? *scale_at : 0.0f;
         float largest = 0.0f;                             // magnitude; as bits, a NaN is above infinity
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        for (int i = 0; i < ITEMS; ++i) {
             if (LAY != ANY) {
 #pragma unroll
                 for (int w = 0; w < 2 * W; ++w) {
@@ -213,13 +213,13 @@ template <int DT, int LAY> __device__ __forceinline__ void append_heads(const Ap
         if (amax * by > 127.4f) {                         // some entry may round beyond 127
             const float most_code = 127.0f * scale;
 #pragma unroll
-            for (int i = 0; i < kItems; ++i)
+            for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[i][j] = fminf(fmaxf(v[i][j], -most_code), most_code);
         }
         int8_t *const to0 = codes + (int64_t)(part.slot + token0) * D;
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        for (int i = 0; i < ITEMS; ++i) {
             if (token0 + i * step >= part.n) break;
             uint32_t w[4];
 #pragma unroll
@@ -246,7 +246,7 @@ template <int DT, int LAY> __device__ __forceinline__ void append_heads(const Ap
     }
 }
 
-template <int DT> __global__ void __launch_bounds__(kAppendMost, 1) append_kernel(const AppendParams P) {
+template <int DT, int ITEMS> __global__ void __launch_bounds__(kAppendMost, 1) append_kernel(const AppendParams P) {
     const int tid = threadIdx.x, which = blockIdx.z;
     let_next();
     wait_before();
@@ -259,10 +259,10 @@ template <int DT> __global__ void __launch_bounds__(kAppendMost, 1) append_kerne
     }
     const int head0 = blockIdx.y * P.heads, head1 = min(head0 + P.heads, P.cache.heads);
     const int R = which == 0 ? P.rotation.rotary : 0;
-    if (!P.vec[which] || (R % 16 && !P.rotation.interleaved)) append_heads<DT, ANY>(P, part, which, head0, head1);
-    else if (R == 0) append_heads<DT, PLAIN>(P, part, which, head0, head1);
-    else if (P.rotation.interleaved) append_heads<DT, PAIRS>(P, part, which, head0, head1);
-    else append_heads<DT, HALVES>(P, part, which, head0, head1);
+    if (!P.vec[which] || (R % 16 && !P.rotation.interleaved)) append_heads<DT, ANY, ITEMS>(P, part, which, head0, head1);
+    else if (R == 0) append_heads<DT, PLAIN, ITEMS>(P, part, which, head0, head1);
+    else if (P.rotation.interleaved) append_heads<DT, PAIRS, ITEMS>(P, part, which, head0, head1);
+    else append_heads<DT, HALVES, ITEMS>(P, part, which, head0, head1);
 }
 
 // ---- read --------------------------------------------------------------------------------------------------------------------
@@ -970,7 +970,10 @@ template <int DT> static Kernels kernels_dt(int dim, int nt) {
 static Kernels kernels_for(const xgen_attention_desc &d, int nt) {
     return d.dtype == XGEN_F32 ? kernels_dt<XGEN_F32>(d.head_dim, nt) : kernels_dt<XGEN_F16_F32ACC>(d.head_dim, nt);
 }
-static const void *append_for(xgen_dtype t) { return t == XGEN_F32 ? (const void *)append_kernel<XGEN_F32> : (const void *)append_kernel<XGEN_F16_F32ACC>; }
+template <int ITEMS> static const void *append_of(xgen_dtype t) {
+    return t == XGEN_F32 ? (const void *)append_kernel<XGEN_F32, ITEMS> : (const void *)append_kernel<XGEN_F16_F32ACC, ITEMS>;
+}
+static const void *append_for(xgen_dtype t, int items) { return items == 2 ? append_of<2>(t) : append_of<4>(t); }
 static const void *read_for(xgen_dtype t) { return t == XGEN_F32 ? (const void *)read_kernel<XGEN_F32> : (const void *)read_kernel<XGEN_F16_F32ACC>; }
 
 // ---- checks ----------------------------------------------------------------------------------------------------------------------
@@ -1155,10 +1158,13 @@ xgen_status xgen_attention_append(const xgen_attention_packed *h, const void *k,
     void *args[] = {&P};
     const int tokens = h->d.page_tokens < b->longest ? h->d.page_tokens : b->longest;
     const int per_token = h->d.head_dim / 16, step = h->d.head_dim % 96 ? 32 : 96;        // threads: whole warps, and whole tokens
-    const int threads = (tokens * per_token + step * kItems - 1) / (step * kItems) * step;
-    P.room = threads * kItems / per_token;
+    // Two items a thread or four, us (with reading back) for 11.6 thousand rows, fp16: 8 heads of 128 in pages of 16 tokens 57 and 69, of 32
+    // 51 and 58, of 64 54 and 47; heads of 64 in pages of 64 32 and 35, of 128 36 and 31.  64 rows: 10.4 and 11.1.
+    const int items = tokens * per_token <= 256 ? 2 : 4;
+    const int threads = (tokens * per_token + step * items - 1) / (step * items) * step;
+    P.room = threads * items / per_token;
     P.heads = heads_of_block(*h, pages, 2);
-    return launch(append_for(h->d.dtype), dim3((unsigned)pages, (h->d.kv_heads + P.heads - 1) / P.heads, 2), dim3(threads), 0, stream, args);
+    return launch(append_for(h->d.dtype, items), dim3((unsigned)pages, (h->d.kv_heads + P.heads - 1) / P.heads, 2), dim3(threads), 0, stream, args);
 }
 
 xgen_status xgen_attention_read(const xgen_attention_packed *h, const xgen_attention_batch *b, const xgen_attention_cache *c, xgen_dtype out_dtype,
