@@ -867,7 +867,7 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
     if (c.units == 0 || c.first == from || c.first < from - c.piece) return;      // no piece; the cut is between two tiles, or not the tile's first
     const int rows = min(MINE, c.n * P.group - c.row0 - first_row);      // of this block's
     if (rows <= 0) return;
-    const int parts = (int)quotient(c.first + c.units - 1, (int)min(c.piece, (int64_t)INT_MAX)) - (worker - 1) + 1;
+    const int parts = (int)quotient(c.first + c.units - 1, c.piece) - (worker - 1) + 1;
     // the first part is its worker's last tile (or all it has), the others are their workers' first
     const int64_t first_slot = (int64_t)(worker - 1) * 2 + (c.first <= from - c.piece ? 0 : 1), next_slot = (int64_t)worker * 2;
     auto slot_of = [&](int part) { return part == 0 ? first_slot : next_slot + 2 * (part - 1); };

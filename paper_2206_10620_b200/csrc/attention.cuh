@@ -121,8 +121,8 @@ __device__ __forceinline__ void mma_bytes(int (&d)[4], const uint32_t (&a)[4], u
 }
 
 // a / b for a >= 0, b > 0: mostly small enough for the short division.
-__device__ __forceinline__ int64_t quotient(int64_t a, int b) {
-    return a < (1ll << 32) ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return (a | b) < (1ll << 32) ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 // What probabilities are multiplied by before they become fp16: it then holds them down to 2^-29 (narrow_kernel) of the largest; 2^-14 of what
 // the row's reference stands for, which the largest may exceed by 2^7 (wide_kernel).

@@ -95,7 +95,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     unsigned char *const probs = values + W::VALUES;                        // fp16 [128 rows][64 tokens], 8 rows of 16 bytes contiguous
     __shared__ float stage_scale[2][2][4];                                  // [stage][keys, values][16 tokens]
     __shared__ unsigned stage_there[2];                                     // which 16 tokens of a stage are in pages that are there
-    __shared__ int units_of[kWideSequences];
+    __shared__ int64_t units_of[kWideSequences];                            // of a key head
     __shared__ int64_t scan[kW + 1], start_units;
     __shared__ int start_s, start_tile, start_unit;
     __shared__ __align__(8) uint64_t bars[5];
@@ -114,9 +114,10 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         const int S = P.batch.sequences;
         for (int i = warp; i < S; i += kW) {
             const WideSequence w = wide_sequence(P, i);
-            int u = 0;
+            int64_t u = 0;
             for (int t = lane; t < w.tiles; t += 32) u += wide_tile(P, w, t).units;
-            u = (int)__reduce_add_sync(~0u, (unsigned)u);
+#pragma unroll
+            for (int d = 16; d; d >>= 1) u += __shfl_xor_sync(~0u, u, d);
             if (lane == 0) units_of[i] = u;
         }
         if (tid == 0) {
@@ -132,7 +133,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         __syncthreads();
         const int each = (S + kWideThreads - 1) / kWideThreads, s0 = min(tid * each, S), s1 = min(s0 + each, S);
         int64_t own = 0;
-        for (int i = s0; i < s1; ++i) own += (int64_t)H * units_of[i];
+        for (int i = s0; i < s1; ++i) own += H * units_of[i];
         int64_t upto = own;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -152,7 +153,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         if (todo > 0 && before <= from && from < before + own) {
             int64_t left = from - before;
             for (int i = s0; i < s1; ++i) {
-                const int64_t u = (int64_t)H * units_of[i];
+                const int64_t u = H * units_of[i];
                 if (left < u) { start_s = i; start_units = left; break; }
                 left -= u;
             }
@@ -166,7 +167,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         q = wide_sequence(P, s);
         head = (int)quotient(start_units, units_of[s]);
         if (warp == 0) {
-            int left = (int)(start_units - (int64_t)head * units_of[s]);
+            int64_t left = start_units - head * units_of[s];
             for (int t0 = 0; t0 < q.tiles; t0 += 32) {
                 const int u = t0 + lane < q.tiles ? wide_tile(P, q, t0 + lane).units : 0;
                 int sum = u;
@@ -178,7 +179,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 const unsigned hit = __ballot_sync(~0u, left < sum);
                 if (hit) {
                     const int at = __ffs(hit) - 1;
-                    if (lane == at) { start_tile = t0 + at; start_unit = left - (sum - u); }
+                    if (lane == at) { start_tile = t0 + at; start_unit = (int)left - (sum - u); }
                     break;
                 }
                 left -= __shfl_sync(~0u, sum, 31);
