@@ -209,13 +209,25 @@ template <int DT, int LAY, int ITEMS> __device__ __forceinline__ void append_hea
                 reinterpret_cast<uint4 *>(codes)[c] = old;
             }
         }
-        const float by = scale > 0.0f ? 1.0f / scale : 0.0f;
+        float by = scale > 0.0f ? 1.0f / scale : 0.0f;
         if (amax * by > 127.4f) {                         // some entry may round beyond 127
             const float most_code = 127.0f * scale;
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[i][j] = fminf(fmaxf(v[i][j], -most_code), most_code);
+        }
+        if ((__float_as_uint(scale) & 0x1FFFu) == 0) {
+            // a scale of few bits: entries of few bits may lie halfway between two codes, and the quotient has to say so (elsewhere they hardly
+            // do, and the product by the reciprocal will do)
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float q = v[i][j] * by;
+                    v[i][j] = fmaf(fmaf(-q, scale, v[i][j]), by, q);
+                }
+            by = 1.0f;
         }
         int8_t *const to0 = codes + (int64_t)(part.slot + token0) * D;
 #pragma unroll

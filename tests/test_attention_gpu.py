@@ -218,6 +218,25 @@ def test_append_zeros_infinities_nan(dtype):
     assert all(torch.isfinite(s[int(pages.table[0, 0])]).all() for s in pages.scale)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("multiple", [1, 3, 5, 7, 9, 15])
+def test_append_entries_halfway_between_codes(dtype, multiple):
+    """They go to the even one: scales of few bits, whose halves an entry can hold."""
+    H, D, page = 1, 128, 64
+    op, freq = make(H, D, page, dtype, rotary=0)
+    pages = su.Pages([page], H, D, page)
+    scale = multiple * 2.0 ** -7
+    x = (torch.arange(page * D, device="cuda") % 253 - 126 + 0.5) * scale
+    x = torch.where((x / 2.0 ** -8).abs() < 2048, x, 0.0)   # (11 bits hold them)
+    x[5] = 127 * scale
+    kv = x.view(page, 1, D).expand(page, 2, D).reshape(page, 2 * D).to(su.T[dtype])
+    append(op, pages, [page], kv, dtype)
+    where = int(pages.table[0, 0])
+    for w in range(2):
+        assert float(pages.scale[w][where, 0]) == scale
+        assert torch.equal(pages.codes[w][where, 0].double(), torch.round(kv[:, :D].double() / scale))
+
+
 def test_append_smallest_and_largest():
     """Entries at the edges of fp32 and of what is normal."""
     op, freq = make(1, 32, 16, "f32", rotary=0)
