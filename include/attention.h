@@ -24,7 +24,7 @@
  *   * otherwise the old scale s is doubled until amax <= 127.5 s, and the older codes of the page are halved as
  *     often, rounded to nearest even.  An entry is then off by less than one step of the page's scale, however often
  *     the page was appended to (the half steps of its roundings are halved each time).
- *   * code = entry / scale rounded to nearest, within -127 .. 127 (by the scale's reciprocal: off by 0.50001 at most).
+ *   * code = entry / scale rounded to nearest, halves to even, within -127 .. 127.
  * A new entry that is not finite makes the page's scale NaN, and it stays NaN until slot 0 is written again: whoever
  * attends to the page (in that head) gets NaN.  Slots behind the sequence's last token are left as they were.
  *

@@ -209,25 +209,13 @@ template <int DT, int LAY, int ITEMS> __device__ __forceinline__ void append_hea
                 reinterpret_cast<uint4 *>(codes)[c] = old;
             }
         }
-        float by = scale > 0.0f ? 1.0f / scale : 0.0f;
+        const float by = scale > 0.0f ? 1.0f / scale : 0.0f;
         if (amax * by > 127.4f) {                         // some entry may round beyond 127
             const float most_code = 127.0f * scale;
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) v[i][j] = fminf(fmaxf(v[i][j], -most_code), most_code);
-        }
-        if ((__float_as_uint(scale) & 0x1FFFu) == 0) {
-            // a scale of few bits: entries of few bits may lie halfway between two codes, and the quotient has to say so (elsewhere they hardly
-            // do, and the product by the reciprocal will do)
-#pragma unroll
-            for (int i = 0; i < ITEMS; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const float q = v[i][j] * by;
-                    v[i][j] = fmaf(fmaf(-q, scale, v[i][j]), by, q);
-                }
-            by = 1.0f;
         }
         int8_t *const to0 = codes + (int64_t)(part.slot + token0) * D;
 #pragma unroll
@@ -238,7 +226,10 @@ template <int DT, int LAY, int ITEMS> __device__ __forceinline__ void append_hea
             for (int j = 0; j < 4; ++j) {
                 uint32_t q[4];                            // 1.5 * 2^23 added leaves the nearest integer in the lowest bits
 #pragma unroll
-                for (int k = 0; k < 4; ++k) q[k] = __float_as_uint(fmaf(v[i][4 * j + k], by, 12582912.0f));
+                for (int k = 0; k < 4; ++k) {             // (the quotient itself: some entries lie halfway between two codes)
+                    const float x = v[i][4 * j + k], about = x * by;
+                    q[k] = __float_as_uint(fmaf(fmaf(-about, scale, x), by, about) + 12582912.0f);
+                }
                 w[j] = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
             }
             if (isnan(scale)) w[0] = w[1] = w[2] = w[3] = 0;
