@@ -57,7 +57,7 @@ xgen_status xgen_adapters_pack(const xgen_adapters_desc *desc, const void *a_hos
  *                 memory that does not overlap y_dev; never memory of x_dev
  * Pointers element-aligned; rows that all start on a multiple of 16 bytes are moved 16 bytes at a time.  Rows that no request owns are
  * neither read nor written.  Row numbers outside 0 .. rows are cut to that range; an adapter number too high
- * counts as none and is reported by xgen_adapters_last_status.
+ * counts as none and, where its request has rows, is reported by xgen_adapters_last_status.
  * Only enqueues one kernel on the stream, on the handle's device; no workspace.  rows = 0 or requests = 0 does nothing.
  * Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (negative sizes, a stride below the
  * row's length, rows or requests above 2^31-1, too many of both for one launch), CUDA.

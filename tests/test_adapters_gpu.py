@@ -175,3 +175,41 @@ def test_captured_and_replayed_with_other_requests():
         torch.cuda.synchronize()
         want, bound = su.adapters(x, y, n, w, a, b, scale, "f16")
         su.close(out, want, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("rows", [40, 400])
+def test_captured_and_on_two_streams(dtype, rows):
+    """Two graphs of one handle, replayed side by side with other requests than they were captured with; rows behind the last are left.
+    An adapter that is not there is reported where its request has rows."""
+    a, b, scale, op = make(dtype, 264, 200, 24, 4)
+    jobs = []
+    for seed in range(2):
+        x = torch.randn((rows, 264), device="cuda", generator=su.gen(seed)).to(su.T[dtype])
+        y = torch.randn((rows, 200), device="cuda", generator=su.gen(seed + 2)).to(su.T[dtype])
+        out = torch.zeros_like(y)
+        start, which = su.starts([rows - 3, 1, 2]), su.ints([0, 1, 2])
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            op.run(x.data_ptr(), rows, 264, start.data_ptr(), which.data_ptr(), 3, y.data_ptr(), 200, out.data_ptr(), 200, torch.cuda.current_stream().cuda_stream)
+        jobs.append((x, y, out, start, which, stream, graph))
+    for n, who in [([rows // 2, 0, rows // 2], [3, 0, -1]), ([1, 1, 1], [2, 1, 0]), ([0, rows, 0], [0, 3, 9]), ([0, 0, 0], [0, 0, 0]), ([2, 3, 4], [0, 9, 3])]:
+        op.sync(su.stream())
+        for x, y, out, start, which, stream, graph in jobs:
+            start.copy_(su.starts(n))
+            which.copy_(su.ints(who))
+            out.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for job in jobs:
+                with torch.cuda.stream(job[5]):
+                    job[6].replay()
+        torch.cuda.synchronize()
+        for x, y, out, *_ in jobs:
+            want, bound = su.adapters(x, y, n, [w if w < 4 else -1 for w in who], a, b, scale, dtype)
+            su.close(out[:sum(n)], want[:sum(n)], bound[:sum(n)])
+            assert (out[sum(n):] == 7.0).all()
+    with pytest.raises(binding.PatconvError) as e:
+        op.sync(su.stream())
+    assert e.value.status == 1
+    op.sync(su.stream())
