@@ -822,14 +822,14 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) row_total[0][8 * n + 2 * t + j] = total[n][j] == 0.0f ? 0.0f : top_unit / (total[n][j] * kLift);
+                    for (int j = 0; j < 2; ++j) row_total[0][8 * n + 2 * t + j] = total[n][j] == 0.0f ? 0.0f : 1.0f / (total[n][j] * kLift);
             }
             __syncthreads();
             for (int i = tid; i < rows * D; i += kThreads) {
                 const int r = i / D, row = (row0 + r) / G, head = now.head * G + (row0 + r) % G;
-                const float by = row_total[0][r];
+                const float by = row_total[0][r];         // (times the unit last: their product need not be a normal number)
                 static_cast<T *>(P.y)[(int64_t)(now.q.row + row) * P.y_stride + (int64_t)head * D + i % D] =
-                    narrow<T>(by == 0.0f ? 0.0f : sum_at(r, i % D) * by);
+                    narrow<T>(by == 0.0f ? 0.0f : sum_at(r, i % D) * by * top_unit);
             }
         } else {
             float *const to = P.partial + ((int64_t)worker * 2 + slot) * ROWS * D;
@@ -860,7 +860,7 @@ constexpr int kCombineThreads = 512, kGroups = 4, kGroup = kCombineThreads / kGr
 template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const RunParams P) {
     using T = typename Elem<DT>::T;
     constexpr int MINE = ROWS < kCombineRows ? ROWS : kCombineRows;
-    __shared__ float4 row_stat[MINE];                     // maximum, unit, factor of the sums
+    __shared__ float4 row_stat[MINE];                     // maximum, unit, factor of the sums (times the unit)
     __shared__ float4 shares[kGroups - 1][kGroup];
     const int worker = blockIdx.x + 1, first_row = blockIdx.y * MINE, tid = threadIdx.x;
     let_next();
@@ -898,15 +898,15 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
             }
 #pragma unroll
             for (int d = 1; d < PER; d <<= 1) total += __shfl_xor_sync(~0u, total, d);
-            if (k == 0) row_stat[r] = make_float4(base, unit, total == 0.0f ? 0.0f : unit / (total * P.lift), 0.0f);
+            if (k == 0) row_stat[r] = make_float4(base, unit, total == 0.0f ? 0.0f : 1.0f / (total * P.lift), 0.0f);
         }
     }
     __syncthreads();
     const auto put = [&](int r, int at, float4 v) {
-        const float by = row_stat[r].z;
+        const float by = row_stat[r].z, unit = row_stat[r].y;
         T *const to = static_cast<T *>(P.y) + (int64_t)(c.row + (c.row0 + first_row + r) / P.group) * P.y_stride +
                       (int64_t)(c.head * P.group + (c.row0 + first_row + r) % P.group) * D + at;
-        const float4 y = by == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
+        const float4 y = by == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * by * unit, v.y * by * unit, v.z * by * unit, v.w * by * unit);
         to[0] = narrow<T>(y.x); to[1] = narrow<T>(y.y); to[2] = narrow<T>(y.z); to[3] = narrow<T>(y.w);
     };
     const auto add = [&](float4 &v, int part, int r, int at) {

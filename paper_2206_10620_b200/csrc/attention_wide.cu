@@ -468,13 +468,15 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                     shrink *= unit / top_scale;
                     unit = top_scale;
                 }
-                const float base = m == -INFINITY ? 0.0f : m, over = unit > 0.0f ? kWideLift / unit : 0.0f;
+                const float base = m == -INFINITY ? 0.0f : m;
                 // ---- probabilities, lifted; totals are of the unlifted ones
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
+                    // (the quotient first: a unit may be as small as fp32's least normal number)
+                    const float lifted = unit > 0.0f ? v_scale[g] / unit * kWideLift : 0.0f;
                     // values of 2^-47 of the largest unit and less are nothing in fp16 (and their lift nothing to divide by)
-                    const bool none = !(v_scale[g] * over >= 1e-12f);
-                    const float lift = none ? 1.0f : v_scale[g] * over, off = log2f(lift) - base;
+                    const bool none = !(lifted >= 1e-12f);
+                    const float lift = none ? 1.0f : lifted, off = log2f(lift) - base;
                     uint32_t hi[8], lo[8];
                     float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
@@ -523,7 +525,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         if (warp < kRowWarps) {
             // ---- the tile's results: a row to a thread
             const bool complete = whole && last_part;
-            const float by = complete ? (l == 0.0f ? 0.0f : unit / (l * kWideLift)) : 1.0f;
+            const float by = complete ? (l == 0.0f ? 0.0f : 1.0f / (l * kWideLift)) : 1.0f, of_unit = complete ? unit : 1.0f;
             T *const y = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + tid) / G) * P.y_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
             float *const part = P.partial + (((int64_t)worker * 2 + slot) * kWideRows + tid) * D;
 #pragma unroll 1
@@ -535,7 +537,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 if (tid < rows) {
                     float x[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = by == 0.0f ? 0.0f : __uint_as_float(r[i]) * by;
+                    for (int i = 0; i < 16; ++i) x[i] = by == 0.0f ? 0.0f : __uint_as_float(r[i]) * by * of_unit;
                     if (!complete) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(part + c * 16)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
