@@ -32,8 +32,10 @@
  * with a window only j > p - window.
  *   y = sum_j softmax_j( softmax_scale * <turned q, k_j> ) v_j
  * A row that sees nothing gives zeros.  Maxima and sums are fp32.  A turned query row becomes integers of 16 bits (fp32
- * layers: 24) times its largest magnitude / 32512 (8323072); their products with the codes are exact.  Probabilities have 11 bits (fp32 layers:
- * 22), relative to the largest of their row so far.
+ * layers: 24) times its largest magnitude / 32512 (8323072); their products with the codes are exact.  What is added
+ * up is the product of a token's probability and its value scale: it has 11 bits down to 2^-20 of the row's largest one so far (fp32 layers:
+ * 22 bits down to 2^-8), and is off by 2^-31 of that largest one at most below.  Pages that the row does not see have no part in it.  A
+ * probability of less than 2^-100 of the row's largest may count as none.
  *
  * Pages outside 0 .. pages-1 (or beyond table_stride) are not touched: appending to one is left out, its
  * tokens are seen by nobody and read as zeros, and xgen_attention_last_status reports it.  A page that is appended to belongs to one

@@ -12,7 +12,7 @@
 // Scores are exact integer products: a query row is a factor times integers of 16 bits (fp32: 24), split into two (three) signed
 // bytes, and integer matrix instructions multiply each with the key codes as they lie in the cache.  Values meet probabilities
 // in fp16 (fp32: in two parts): a code is exact there, widened by byte permutes and one subtraction.  The page's scales are
-// applied to scores and probabilities in fp32.
+// applied to scores and probabilities in fp32; attention.cuh says relative to what the latter become fp16.
 #include <cmath>
 #include <climits>
 #include <cstring>
@@ -433,7 +433,7 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
     float *const sums = reinterpret_cast<float *>(shared + N::RING + N::Q_BYTES);        // [COPIES][ROWS][SUM_ROW]
     __shared__ float stage_scale[kWarps][N::STAGES][2];
     __shared__ float row_factor[ROWS];
-    __shared__ float row_most[kWarps][ROWS], row_total[kWarps][ROWS], warp_unit[kWarps];
+    __shared__ float row_most[kWarps][ROWS], row_total[kWarps][ROWS], row_unit[kWarps][ROWS];
     __shared__ int64_t scan[kWarps + 1], start_units;
     __shared__ int start_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -644,10 +644,10 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
 
         // o[n][c]: components 16c + 2g of rows 8n + 2t and 8n + 2t + 1, then component 16c + 2g + 1 of both
         float o[NT][D / 16][4];
-        float m[NT][2], l[NT][2], unit = 0.0f;             // unit: the values' scale that o is in
+        float m[NT][2], l[NT][2], unit[NT][2];             // (attention.cuh)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            m[n][0] = m[n][1] = -INFINITY;
+            m[n][0] = m[n][1] = unit[n][0] = unit[n][1] = -INFINITY;
             l[n][0] = l[n][1] = 0.0f;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) o[n][c][0] = o[n][c][1] = o[n][c][2] = o[n][c][3] = 0.0f;
@@ -677,58 +677,79 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
                             else mma_bytes(dot[k][n], a, query(k, n, c, 0), query(k, n, c, 1));
                         }
                 }
-                // scores in powers of two, what a row does not see out of them, the running maximum (rows: g and g + 8 of the tokens)
+                // scores in powers of two less the reference, what a row does not see out of them (rows: g and g + 8 of the tokens)
                 const bool all_seen = token + kTokens - 1 <= least_position && P.window == 0;       // (what the rows behind the last one see is no matter)
-                float s[NT][4], shrink[NT][2], most[NT][2];
-                bool changed = false;
+                const Split value = split_scale(v_scale);
+                float s[NT][4], by[NT][2];
+                bool rise = false;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
+                    float base[2], limit[2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        base[j] = m[n][j] == -INFINITY ? 0.0f : m[n][j];
+                        limit[j] = m[n][j] == -INFINITY ? -INFINITY : kFar + fminf(unit[n][j] - value.e, 0.0f);
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int j = token + g + 8 * (i >> 1), p = position[n][i & 1];
                         float x = TERMS == 3 ? fmaf((float)dot[TERMS - 1][n][i], 65536.0f, (float)(dot[1][n][i] * 256 + dot[0][n][i]))
                                              : (float)(dot[1][n][i] * 256 + dot[0][n][i]);
-                        x *= k_scale * factor[n][i & 1];
+                        x = fmaf(x, k_scale * factor[n][i & 1], -base[i & 1]);
                         if (!all_seen && (j > p || (P.window > 0 && j <= p - P.window))) x = -INFINITY;
                         s[n][i] = x;
+                        rise |= x > limit[i & 1];
                     }
+                }
+                const bool lost = !(v_scale < INFINITY);
+                if (__any_sync(~0u, rise || lost)) {       // references go up; the rows that see some of a lost page are lost, the others are not
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float shrink[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float x = max_or_nan(s[n][j], s[n][2 + j]);
+#pragma unroll
+                            for (int d = 4; d < 32; d <<= 1) x = max_or_nan(x, __shfl_xor_sync(~0u, x, d));
+                            if (lost && !(x == -INFINITY)) l[n][j] = NAN;
+                            const bool first = m[n][j] == -INFINITY;
+                            if (x > (first ? -INFINITY : kFar)) {
+                                const float up = raise_reference(m[n][j], first ? 0.0f : m[n][j], x);
+                                if (!first) l[n][j] *= exp2_approx(-up);
+                                unit[n][j] -= up;
+                                x -= up;
+                                s[n][j] -= up;
+                                s[n][2 + j] -= up;
+                            }
+                            const float weight = x > -100.0f ? ceilf(x + value.e) : -INFINITY;
+                            shrink[j] = 1.0f;
+                            if (weight > unit[n][j] + kFar) {
+                                shrink[j] = exp2_approx(unit[n][j] - weight);
+                                unit[n][j] = weight;
+                            }
+                        }
+#pragma unroll
+                        for (int c = 0; c < D / 16; ++c) {
+                            o[n][c][0] *= shrink[0]; o[n][c][1] *= shrink[1]; o[n][c][2] *= shrink[0]; o[n][c][3] *= shrink[1];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        float x = max_or_nan(s[n][j], s[n][2 + j]);
+                        const float far = value.e - unit[n][j];
+                        by[n][j] = far <= 100.0f ? value.f * exp2_approx(far + (float)kLift) : 0.0f;
 #pragma unroll
-                        for (int d = 4; d < 32; d <<= 1) x = max_or_nan(x, __shfl_xor_sync(~0u, x, d));
-                        most[n][j] = x;
-                        x = max_or_nan(m[n][j], x);
-                        const float base = x == -INFINITY ? 0.0f : x;
-                        shrink[n][j] = exp2_approx(m[n][j] - base);
-                        m[n][j] = x;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) s[n][2 * i + j] = exp2_approx(s[n][2 * i + j] - base);
-                        l[n][j] = l[n][j] * shrink[n][j] + (s[n][j] + s[n][2 + j]);
+                        for (int i = 0; i < 2; ++i) s[n][2 * i + j] = exp2_approx(s[n][2 * i + j]);
+                        l[n][j] += s[n][j] + s[n][2 + j];
                     }
-                }
-                // probabilities times 2^15 (fp16 then holds them down to 2^-29 of the largest), values relative to the largest scale
-                float by = kLift;
-                if (v_scale > unit && v_scale < INFINITY) {
-                    const float x = unit / v_scale;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) { shrink[n][0] *= x; shrink[n][1] *= x; }
-                    unit = v_scale;
-                } else if (v_scale != unit && unit > 0.0f) by = v_scale < INFINITY ? kLift * (v_scale / unit) : 0.0f;
-                if (!(v_scale < INFINITY)) {               // the rows that see some of the page are lost, the others are not
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            if (!(most[n][j] == -INFINITY)) l[n][j] = NAN;
-                }
                 uint32_t p[NT][2], p_low[NT][2];           // as the second operand: rows (tokens) 2t .. and 2t + 8 .., column (query row) g
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    changed |= shrink[n][0] != 1.0f || shrink[n][1] != 1.0f;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float x0 = s[n][2 * i] * by, x1 = s[n][2 * i + 1] * by;
+                        const float x0 = s[n][2 * i] * by[n][0], x1 = s[n][2 * i + 1] * by[n][1];
                         const uint32_t high = pack_half(x0, x1);
                         p[n][i] = turn_matrix(high);
                         if (N::SPLIT) {
@@ -736,14 +757,6 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
                             p_low[n][i] = turn_matrix(pack_half(x0 - __low2float(h), x1 - __high2float(h)));
                         }
                     }
-                }
-                if (__any_sync(~0u, changed)) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int c = 0; c < D / 16; ++c) {
-                            o[n][c][0] *= shrink[n][0]; o[n][c][1] *= shrink[n][1]; o[n][c][2] *= shrink[n][0]; o[n][c][3] *= shrink[n][1];
-                        }
                 }
 #pragma unroll
                 for (int c = 0; c < D / 16; c += 2) {
@@ -777,13 +790,10 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) l[n][j] += __shfl_xor_sync(~0u, l[n][j], d);
-                if (g == 0) { row_most[warp][8 * n + 2 * t + j] = m[n][j]; row_total[warp][8 * n + 2 * t + j] = l[n][j]; }
+                if (g == 0) { row_most[warp][8 * n + 2 * t + j] = m[n][j]; row_total[warp][8 * n + 2 * t + j] = l[n][j]; row_unit[warp][8 * n + 2 * t + j] = unit[n][j]; }
             }
-        if (lane == 0) warp_unit[warp] = unit;
         __syncthreads();
-        float top[NT][2], total[NT][2], mine[NT][2], top_unit = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) top_unit = fmaxf(top_unit, warp_unit[w]);
+        float top[NT][2], total[NT][2], mine[NT][2], top_unit[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -794,9 +804,13 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
                 for (int w = 1; w < kWarps; ++w) top[n][j] = max_or_nan(top[n][j], row_most[w][r]);
                 const float base = top[n][j] == -INFINITY ? 0.0f : top[n][j];
                 total[n][j] = 0.0f;
+                top_unit[n][j] = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) total[n][j] += row_total[w][r] * exp2_approx(row_most[w][r] - base);
-                mine[n][j] = unit == 0.0f ? 0.0f : exp2_approx(m[n][j] - base) * (unit / top_unit);
+                for (int w = 0; w < kWarps; ++w) {
+                    total[n][j] += row_total[w][r] * exp2_approx(row_most[w][r] - base);
+                    top_unit[n][j] = fmaxf(top_unit[n][j], row_most[w][r] - base + row_unit[w][r]);
+                }
+                mine[n][j] = unit[n][j] == -INFINITY ? 0.0f : exp2_approx(m[n][j] - base + unit[n][j] - top_unit[n][j]);
             }
         for (int w = 0; w < kWarps / N::COPIES; ++w) {
             if (warp / N::COPIES == w) {
@@ -822,14 +836,18 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) row_total[0][8 * n + 2 * t + j] = total[n][j] == 0.0f ? 0.0f : 1.0f / (total[n][j] * kLift);
+                    for (int j = 0; j < 2; ++j) {
+                        const float2 f = result_factors(total[n][j], top_unit[n][j]);
+                        row_total[0][8 * n + 2 * t + j] = f.x;
+                        row_unit[0][8 * n + 2 * t + j] = f.y;
+                    }
             }
             __syncthreads();
             for (int i = tid; i < rows * D; i += kThreads) {
                 const int r = i / D, row = (row0 + r) / G, head = now.head * G + (row0 + r) % G;
-                const float by = row_total[0][r];         // (times the unit last: their product need not be a normal number)
+                const float by = row_total[0][r];
                 static_cast<T *>(P.y)[(int64_t)(now.q.row + row) * P.y_stride + (int64_t)head * D + i % D] =
-                    narrow<T>(by == 0.0f ? 0.0f : sum_at(r, i % D) * by * top_unit);
+                    narrow<T>(by == 0.0f ? 0.0f : sum_at(r, i % D) * by * row_unit[0][r]);
             }
         } else {
             float *const to = P.partial + ((int64_t)worker * 2 + slot) * ROWS * D;
@@ -839,7 +857,7 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        P.stats[((int64_t)worker * 2 + slot) * ROWS + 8 * n + 2 * t + j] = make_float4(top[n][j], total[n][j], top_unit, 0.0f);
+                        P.stats[((int64_t)worker * 2 + slot) * ROWS + 8 * n + 2 * t + j] = make_float4(top[n][j], total[n][j], top_unit[n][j], 0.0f);
             }
         }
         __syncthreads();
@@ -860,7 +878,7 @@ constexpr int kCombineThreads = 512, kGroups = 4, kGroup = kCombineThreads / kGr
 template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThreads) combine_kernel(const RunParams P) {
     using T = typename Elem<DT>::T;
     constexpr int MINE = ROWS < kCombineRows ? ROWS : kCombineRows;
-    __shared__ float4 row_stat[MINE];                     // maximum, unit, factor of the sums (times the unit)
+    __shared__ float4 row_stat[MINE];                     // reference, unit, the sums' two factors
     __shared__ float4 shares[kGroups - 1][kGroup];
     const int worker = blockIdx.x + 1, first_row = blockIdx.y * MINE, tid = threadIdx.x;
     let_next();
@@ -879,31 +897,29 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
         constexpr int PER = 32;
         const int r = tid / PER, k = tid % PER;
         if (r < rows) {
-            float top = -INFINITY, unit = 0.0f;
-            for (int part = k; part < parts; part += PER) {
-                const float4 x = P.stats[slot_of(part) * ROWS + first_row + r];
-                top = max_or_nan(top, x.x);
-                unit = fmaxf(unit, x.z);
-            }
+            float top = -INFINITY;
+            for (int part = k; part < parts; part += PER) top = max_or_nan(top, P.stats[slot_of(part) * ROWS + first_row + r].x);
 #pragma unroll
-            for (int d = 1; d < PER; d <<= 1) {
-                top = max_or_nan(top, __shfl_xor_sync(~0u, top, d));
-                unit = fmaxf(unit, __shfl_xor_sync(~0u, unit, d));
-            }
+            for (int d = 1; d < PER; d <<= 1) top = max_or_nan(top, __shfl_xor_sync(~0u, top, d));
             const float base = top == -INFINITY ? 0.0f : top;
-            float total = 0.0f;
+            float total = 0.0f, unit = -INFINITY;
             for (int part = k; part < parts; part += PER) {
                 const float4 x = P.stats[slot_of(part) * ROWS + first_row + r];
                 total += exp2_approx(x.x - base) * x.y;
+                unit = fmaxf(unit, x.x - base + x.z);
             }
 #pragma unroll
-            for (int d = 1; d < PER; d <<= 1) total += __shfl_xor_sync(~0u, total, d);
-            if (k == 0) row_stat[r] = make_float4(base, unit, total == 0.0f ? 0.0f : 1.0f / (total * P.lift), 0.0f);
+            for (int d = 1; d < PER; d <<= 1) {
+                total += __shfl_xor_sync(~0u, total, d);
+                unit = fmaxf(unit, __shfl_xor_sync(~0u, unit, d));
+            }
+            const float2 f = result_factors(total, unit);
+            if (k == 0) row_stat[r] = make_float4(base, unit, f.x, f.y);
         }
     }
     __syncthreads();
     const auto put = [&](int r, int at, float4 v) {
-        const float by = row_stat[r].z, unit = row_stat[r].y;
+        const float by = row_stat[r].z, unit = row_stat[r].w;
         T *const to = static_cast<T *>(P.y) + (int64_t)(c.row + (c.row0 + first_row + r) / P.group) * P.y_stride +
                       (int64_t)(c.head * P.group + (c.row0 + first_row + r) % P.group) * D + at;
         const float4 y = by == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(v.x * by * unit, v.y * by * unit, v.z * by * unit, v.w * by * unit);
@@ -914,7 +930,7 @@ template <int DT, int D, int ROWS> __global__ void __launch_bounds__(kCombineThr
         const float4 x = P.stats[slot * ROWS + first_row + r];
         const float4 o = *reinterpret_cast<const float4 *>(P.partial + (slot * ROWS + first_row + r) * D + at);
         const float4 stat = row_stat[r];
-        const float f = x.z == 0.0f ? 0.0f : exp2_approx(x.x - stat.x) * (x.z / stat.y);
+        const float f = x.z == -INFINITY ? 0.0f : exp2_approx(x.x - stat.x + x.z - stat.y);
         v.x += f * o.x; v.y += f * o.y; v.z += f * o.z; v.w += f * o.w;
     };
     if (parts <= kGroups) {                               // a thread adds up all parts of what it has
@@ -1239,7 +1255,6 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     // a kernel over tiles of `rows` rows, and the joining of what its workers leave in pieces
     const auto attend = [&](const void *kernel, const void *combine, int workers, int rows, int threads, int shared, char *work) {
         P.workers = workers;
-        P.lift = rows == kWideRows ? kWideLift : kLift;
         P.partial = reinterpret_cast<float *>(work);
         P.stats = reinterpret_cast<float4 *>(P.partial + (int64_t)workers * 2 * rows * h->d.head_dim);
         P.cut = reinterpret_cast<Cut *>(P.stats + (int64_t)workers * 2 * rows);

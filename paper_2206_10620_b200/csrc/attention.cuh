@@ -124,9 +124,35 @@ __device__ __forceinline__ void mma_bytes(int (&d)[4], const uint32_t (&a)[4], u
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
     return (a | b) < (1ll << 32) ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// What probabilities are multiplied by before they become fp16: it then holds them down to 2^-29 (narrow_kernel) of the largest; 2^-14 of what
-// the row's reference stands for, which the largest may exceed by 2^7 (wide_kernel).
-constexpr float kLift = 32768.0f, kWideLift = 128.0f;
+// A row's sums are of probability times scale times code.  What goes into fp16 is the product of the first two, relative to the largest that
+// the row has met so far, not the probability relative to the largest scale: a page of large values that hardly counts for the row, or that
+// it does not see, must not cost the others their bits.  (Relative to the largest scale, a page 10^6 times smaller with all the weight kept
+// 12 bits of the 22 in fp32 layers.)
+// The row keeps, as whole numbers of powers of two, so that changing them rounds nothing, a reference m of its scores and one of its
+// sums, `unit`, relative to m: sums are of p f 2^(e + kLift - unit) code for a scale f 2^e, p = 2^(score - m); -infinity: no sums yet.
+// They go up where a score, or a product, lies more than 2^kFar above them.  So a product is at most 2^15 as it becomes fp16, which holds
+// all its bits down to 2^-20 of the row's largest.  A probability of less than 2^-100 of the row's largest may count as none.
+// (Scores are formed relative to m, in one rounding, so that far from 0 too they are no further above it than they are said to be.)
+constexpr int kLift = 7;
+constexpr float kFar = 7.0f;
+// A scale as f times 2^e, 1 <= f < 2; e = -infinity for one that is not above 0, or not finite.
+struct Split { float e, f; };
+__device__ __forceinline__ Split split_scale(float v) {
+    const bool least = v < 1.17549435e-38f;               // below the normal numbers
+    const uint32_t u = __float_as_uint(least ? v * 4294967296.0f : v);
+    if (!(v > 0.0f && v < INFINITY)) return {-INFINITY, 1.0f};
+    return {(float)((int)(u >> 23) - (least ? 159 : 127)), __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u)};
+}
+// The score reference once more where the largest score lies x above `base`; by how much it went up.  (Rounded up, where it has no room for units.)
+__device__ __forceinline__ float raise_reference(float &m, float base, float x) {
+    m = __fadd_ru(base, ceilf(x));
+    return m - base;
+}
+// What a row's sums are to be multiplied by, one after the other (their product may not be a normal number): 2^(unit - kLift) / total.
+__device__ __forceinline__ float2 result_factors(float total, float unit) {
+    const float near = fminf(fmaxf(unit, -126.0f), 127.0f);
+    return make_float2(total == 0.0f ? 0.0f : pow2(-kLift) / total * exp2_approx(unit - near), exp2_approx(near));
+}
 
 // Where a worker's piece of the line begins: the tile (its rows, the units that it takes, which unit of the line is its first), and the
 // length of a piece.
@@ -143,9 +169,9 @@ struct RunParams {
     int64_t q_stride, y_stride;
     int group, window;
     bool vec_y;                      // rows of y start on multiples of 16 bytes
-    float scale, lift;               // softmax scale times log2(e); what the kernel's probabilities are multiplied by
+    float scale;                     // softmax scale times log2(e)
     float *partial;                  // [workers][2][rows of a tile][dim] sums
-    float4 *stats;                   // [workers][2][rows of a tile]: maximum, total, unit of the sums
+    float4 *stats;                   // [workers][2][rows of a tile]: reference m, total, unit of the sums
     struct Cut *cut;                 // [workers]
     int8_t *q_bytes;                 // wide_kernel: [kv_heads][rows * group][terms][dim]: the queries' integers, bytes of the lowest value first
     float *q_factor;                 // [kv_heads][rows * group]: what they are multiples of, times the scale

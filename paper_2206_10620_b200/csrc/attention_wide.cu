@@ -6,8 +6,8 @@
 //     accumulator per byte; a thread reads its row's 64 integers and has its softmax without any exchange;
 //   * probabilities go to shared memory as fp16 (fp32: in two parts), value codes are widened to fp16 there, rows of tokens being the
 //     contiguous direction (the operand is given as transposed), and kind::f16 adds their product to the sums.
-// The sums are rescaled only where a row's maximum rises by more than 2^7 (or the values' scale doubles): probabilities are
-// lifted by 2^7, so that fp16 holds what that leaves.
+// The sums are rescaled only where a row's largest product of probability and scale rises by more than 2^7: what goes into fp16
+// is lifted by 2^7, so that it holds what that leaves (attention.cuh).
 // A warp of its own copies the codes, two steps ahead, and issues the matrix instructions, the product of step j and the scores of step
 // j + 1 back to back; meanwhile the threads widen the values of step j + 1.  They meet that warp alone (barriers in shared memory), not
 // one another.  Two blocks to an SM fill each other's gaps.
@@ -38,7 +38,6 @@ using patconv::tmem_wait_ld;
 using patconv::tmem_wait_st;
 
 constexpr int kRowWarps = kWideRows / 32, kW = kRowWarps + 1;      // warps that own rows; the last one copies and issues
-constexpr float kFar = 7.0f;                              // (2^7 * 2^7 * 2, for values up to twice the unit, is within fp16)
 
 template <int DT, int D> struct Wide {
     static constexpr bool SPLIT = DT == XGEN_F32;
@@ -94,7 +93,8 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     unsigned char *const values = codes + 4 * W::CODES;                     // fp16 [8 tokens of 16 bytes][D/8][8]
     unsigned char *const probs = values + W::VALUES;                        // fp16 [128 rows][64 tokens], 8 rows of 16 bytes contiguous
     __shared__ float stage_scale[2][2][4];                                  // [stage][keys, values][16 tokens]
-    __shared__ unsigned stage_there[2];                                     // which 16 tokens of a stage are in pages that are there
+    __shared__ float4 stage_value[2][4];                                    // of the values' scales: exponent, kLift plus log2 of the rest, reciprocal of both
+    __shared__ unsigned stage_there[2];                                     // which 16 tokens of a stage are in pages that are there (bits 0-3), with a lost scale (4-7)
     __shared__ int64_t units_of[kWideSequences];                            // of a key head
     __shared__ int64_t scan[kW + 1], start_units;
     __shared__ int start_s, start_tile, start_unit;
@@ -253,7 +253,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         const int row0 = tile * kWideRows, rows = min(kWideRows, q.n * G - row0), before = q.length - q.n;
         const int units = (int)min(todo, (int64_t)(w.units - skipped));
         const bool last_part = skipped + units == w.units;
-        float l = 0.0f, m = -INFINITY, unit = 0.0f, since = 1.0f;       // since: what the totals are to be multiplied by
+        float l = 0.0f, m = -INFINITY, unit = -INFINITY, since = 1.0f;       // since: what the totals are to be multiplied by
         if (warp == kRowWarps) {
             // ---- codes, two steps ahead; matrix instructions, whenever the threads are done with a step (first: with the queries)
             const int token_begin = w.from + (int)skipped * kWideUnit;
@@ -303,8 +303,17 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             for (int u = -1; u < units; ++u) {
                 if (u + 1 < units) {                      // the next step's codes are there
                     if (u < 0) copy_async_wait<1>(); else copy_async_wait<0>();
+                    const int stage = (phase_c + u + 1) & 1;
+                    const unsigned there = stage_there[stage];
+                    const float v = lane < 4 && there >> lane & 1 ? stage_scale[stage][1][lane] : 0.0f;      // (what this lane copied itself)
+                    const unsigned lost = __ballot_sync(~0u, !(v < INFINITY));
+                    if (lane < 4) {
+                        const Split f = split_scale(v);
+                        stage_value[stage][lane] = make_float4(f.e, (float)kLift + log2f(f.f), pow2(-kLift) / f.f, 0.0f);
+                    }
+                    if (lost && lane == 0) stage_there[stage] = there | lost << 4;
                     fence_async_proxy();
-                    patconv::mbar_arrive(bar_c + 8 * ((phase_c + u + 1) & 1));
+                    patconv::mbar_arrive(bar_c + 8 * stage);
                 }
                 mbar_wait<false>(bar_p, (uint32_t)(phase_p & 1), &s_abort, timeout, 2000000u);
                 ++phase_p;
@@ -362,10 +371,28 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 const int stage = phase_c & 1, token = token_begin + u * kWideUnit;
                 mbar_wait<false>(bar_c + 8 * stage, (uint32_t)(phase_c >> 1 & 1), &s_abort, timeout, 2000000u);
                 ++phase_c;
-                const unsigned there = stage_there[stage];
-                float k_scale[4], v_scale[4];
+                const unsigned there = stage_there[stage] & 15u, lost = stage_there[stage] >> 4;
+                float k_scale[4];
 #pragma unroll
-                for (int g = 0; g < 4; ++g) { k_scale[g] = stage_scale[stage][0][g]; v_scale[g] = stage_scale[stage][1][g]; }
+                for (int g = 0; g < 4; ++g) k_scale[g] = stage_scale[stage][0][g];
+                // Of 16 tokens each: what is added to a score so that its power of two is the product of probability and scale, lifted; what the
+                // sum of these is multiplied by to be one of probabilities; the score from which on references go up.  What is 2^-45 of the
+                // reference or less is nothing in fp16, wherever below that it is put, but its probability counts.
+                // Scores are less m in fp32 layers (in the rounding that they have anyway); in fp16 layers, where that took 3 % longer, m is in
+                // what is added, rounded down: far from 0, where that is by many units, a product must not come out above 2^15.
+                float off[4], plain[4], limit[4], base;
+                const auto prepare = [&] {
+                    base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const float4 value = stage_value[stage][g];
+                        const float far = fminf(fmaxf(value.x - unit, -45.0f), 110.0f), reach = kFar + fminf(unit - value.x, 0.0f);
+                        off[g] = W::SPLIT ? far + value.y : __fadd_rd(far + value.y, -base);
+                        plain[g] = exp2_approx(-far) * value.z;
+                        limit[g] = !W::SPLIT ? __fadd_rd(m, reach) : m == -INFINITY ? -INFINITY : reach;
+                    }
+                };
+                prepare();
                 // ---- values to fp16
                 {
                     const unsigned char *const from = codes + stage * 2 * W::CODES + W::CODES;
@@ -418,7 +445,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         const float by = k_scale[c] * factor;
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            sc[c * 16 + i] = by * fmaf((float)(int)r[2][i], 65536.0f, (float)((int)r[1][i] * 256 + (int)r[0][i]));
+                            sc[c * 16 + i] = fmaf(fmaf((float)(int)r[2][i], 65536.0f, (float)((int)r[1][i] * 256 + (int)r[0][i])), by, -base);
                     } else {
                         // an integer of less than 23 bits as the low bits of 1.5 * 2^23 (a conversion would take the exponentials' unit)
                         const float by = k_scale[c] * factor * (float)(1 << W::DROP), less = -12582912.0f * by;
@@ -446,42 +473,55 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
 #pragma unroll
                     for (int i = 2; i < 16; i += 2) most[g] = max_or_nan(most[g], sc[16 * g + i], sc[16 * g + i + 1]);
                 }
-                const float largest = max_or_nan(max_or_nan(most[0], most[1]), max_or_nan(most[2], most[3]));
-                // ---- the row's reference, the values' unit
+                // ---- the row's references go up; a NaN goes into l (what the row does not see has a score of -infinity)
                 float shrink = 1.0f;
-                if (!(largest <= m + kFar)) {             // (from -infinity too; a NaN stays in l)
-                    shrink = exp2_approx(m - largest);
-                    m = largest;
-                }
-                l *= shrink;
-                float top_scale = 0.0f;
+                if (__any_sync(~0u, most[0] > limit[0] || most[1] > limit[1] || most[2] > limit[2] || most[3] > limit[3])) {
+                    const float largest = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                    float heaviest = -INFINITY;
+                    if constexpr (W::SPLIT) {
+                        const bool first = m == -INFINITY;
+                        float up = 0.0f;
+                        if (largest > (first ? -INFINITY : kFar)) {
+                            up = raise_reference(m, base, largest);
+                            if (!first) l *= exp2_approx(-up);
+                            unit -= up;
+                        }
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    if (!(there >> g & 1)) v_scale[g] = 0.0f;
-                    if (!(v_scale[g] < INFINITY)) {       // the rows that see some of a lost page are lost, the others are not
-                        if (token + 16 * g <= position && (P.window == 0 || token + 16 * g + 15 > position - P.window)) l = NAN;
-                        v_scale[g] = 0.0f;
+                        for (int i = 0; i < kWideUnit; ++i) sc[i] -= up;
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            if (most[g] - up > -100.0f) heaviest = fmaxf(heaviest, most[g] - up + stage_value[stage][g].x);
+                    } else {
+                        if (largest > m + kFar) {
+                            const float to = ceilf(largest);
+                            l *= exp2_approx(m - to);
+                            unit -= to - m;
+                            m = to;
+                        }
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            if (most[g] - m > -100.0f) heaviest = fmaxf(heaviest, most[g] - m + stage_value[stage][g].x);
                     }
-                    top_scale = fmaxf(top_scale, v_scale[g]);
+                    if (heaviest > unit + kFar) {
+                        const float to = ceilf(heaviest);
+                        shrink = exp2_approx(unit - to);
+                        unit = to;
+                    }
+                    prepare();
                 }
-                if (top_scale > 2.0f * unit) {
-                    shrink *= unit / top_scale;
-                    unit = top_scale;
+                if (lost) {                               // the rows that see some of a lost page are lost, the others are not
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        if (lost >> g & 1 && !(most[g] == -INFINITY)) l = NAN;
                 }
-                const float base = m == -INFINITY ? 0.0f : m;
-                // ---- probabilities, lifted; totals are of the unlifted ones
+                // ---- products of probabilities and scales, lifted; totals are of the probabilities alone
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    // (the quotient first: a unit may be as small as fp32's least normal number)
-                    const float lifted = unit > 0.0f ? v_scale[g] / unit * kWideLift : 0.0f;
-                    // values of 2^-47 of the largest unit and less are nothing in fp16 (and their lift nothing to divide by)
-                    const bool none = !(lifted >= 1e-12f);
-                    const float lift = none ? 1.0f : lifted, off = log2f(lift) - base;
                     uint32_t hi[8], lo[8];
                     float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float x0 = exp2_approx(sc[16 * g + 2 * i] + off), x1 = exp2_approx(sc[16 * g + 2 * i + 1] + off);
+                        const float x0 = exp2_approx(sc[16 * g + 2 * i] + off[g]), x1 = exp2_approx(sc[16 * g + 2 * i + 1] + off[g]);
                         sum0 += x0;
                         sum1 += x1;
                         hi[i] = pack_half(x0, x1);
@@ -490,11 +530,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                             lo[i] = pack_half(x0 - __low2float(h), x1 - __high2float(h));
                         }
                     }
-                    l += __fdividef(sum0 + sum1, lift);
-                    if (none) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) hi[i] = lo[i] = 0;
-                    }
+                    l = fmaf(sum0 + sum1, plain[g], l);
                     uint4 *const to = reinterpret_cast<uint4 *>(probs + (tid >> 3) * (kWideUnit * 16) + g * 256 + (tid & 7) * 16);
                     to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                     to[8] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
@@ -525,7 +561,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
         if (warp < kRowWarps) {
             // ---- the tile's results: a row to a thread
             const bool complete = whole && last_part;
-            const float by = complete ? (l == 0.0f ? 0.0f : 1.0f / (l * kWideLift)) : 1.0f, of_unit = complete ? unit : 1.0f;
+            const float2 f = complete ? result_factors(l, unit) : make_float2(1.0f, 1.0f);
             T *const y = static_cast<T *>(P.y) + (int64_t)(q.row + (row0 + tid) / G) * P.y_stride + (int64_t)(head * G + (row0 + tid) % G) * D;
             float *const part = P.partial + (((int64_t)worker * 2 + slot) * kWideRows + tid) * D;
 #pragma unroll 1
@@ -537,7 +573,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 if (tid < rows) {
                     float x[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = by == 0.0f ? 0.0f : __uint_as_float(r[i]) * by * of_unit;
+                    for (int i = 0; i < 16; ++i) x[i] = f.x == 0.0f ? 0.0f : __uint_as_float(r[i]) * f.x * f.y;
                     if (!complete) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) reinterpret_cast<float4 *>(part + c * 16)[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
