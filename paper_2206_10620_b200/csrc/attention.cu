@@ -357,6 +357,10 @@ template <int DT> __global__ void __launch_bounds__(kReadThreads, 5) read_kernel
 // ---- run: few rows against a long cache ------------------------------------------------------------------------------------------
 constexpr int kTokens = 16;          // tokens that a warp takes at a time, in one page
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kUnit = kWarps * kTokens;
+// fp16 layers: units that a tile goes on with the same sums.  The matrix unit rounds them toward zero, 2^-23 at most with every unit: over 4096
+// units a row's values were short of an fp16 step, over 16384 of two.  (fp32 layers add up with rounding, at every 16 tokens; as much
+// takes one request over 1000 tokens from 10.8 us to 12.9 here.)
+constexpr int kUnitsOnce = 512;
 
 
 // What a sequence asks for: rows, tiles of rows for each key head, units of a tile, where its tokens begin.
@@ -558,7 +562,7 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
 
     int stage = 0;
     const uint32_t a_lane = (uint32_t)((lane & 7) + (lane & 8)) * N::ROW + (lane >> 4) * 16;     // this lane's row of four matrices
-    bool whole = skipped == 0;
+    bool whole = skipped == 0, held = false;               // held: the partial results' place has what came of the tile's units so far
     int slot = 0;                                          // of the partial results: 0 for the piece's first tile
     while (todo > 0) {
         // ---- one tile of rows: queries, turned, as a factor times integers
@@ -654,7 +658,7 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
         }
 
         // ---- its tokens, as far as the piece goes
-        const int units = (int)min(todo, (int64_t)(now.q.units - now.unit));
+        const int units = (int)min(todo, (int64_t)(N::SPLIT ? now.q.units - now.unit : min(now.q.units - now.unit, kUnitsOnce)));
         const bool last_part = now.unit + units == now.q.units;
         int token = token_of(now);
         for (int u = 0; u < units; ++u, token += kUnit) {
@@ -829,7 +833,32 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
             }
             __syncthreads();
         }
-        auto sum_at = [&](int r, int d) { return N::COPIES == 1 ? sums[r * N::SUM_ROW + d] : sums[r * N::SUM_ROW + d] + sums[N::SUMS + r * N::SUM_ROW + d]; };
+        float *const partial = P.partial + ((int64_t)worker * 2 + slot) * ROWS * D;
+        float4 *const stats = P.stats + ((int64_t)worker * 2 + slot) * ROWS;
+        if (!N::SPLIT && held) {                           // what both count for: row_most[1], [2]
+            if (warp == 0 && g == 0) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int r = 8 * n + 2 * t + j;
+                        const float4 old = stats[r];
+                        const float both = max_or_nan(top[n][j], old.x), base = both == -INFINITY ? 0.0f : both;
+                        const float mine = top[n][j] - base + top_unit[n][j], theirs = old.x - base + old.z, unit = fmaxf(mine, theirs);
+                        total[n][j] = total[n][j] * exp2_approx(top[n][j] - base) + old.y * exp2_approx(old.x - base);
+                        row_most[1][r] = top_unit[n][j] == -INFINITY ? 0.0f : exp2_approx(mine - unit);
+                        row_most[2][r] = old.z == -INFINITY ? 0.0f : exp2_approx(theirs - unit);
+                        top[n][j] = both;
+                        top_unit[n][j] = unit;
+                    }
+            }
+            __syncthreads();
+        }
+        auto sum_at = [&](int i) {                         // element i of the tile (always the same thread's)
+            const int r = i / D, at = r * N::SUM_ROW + i % D;
+            const float v = N::COPIES == 1 ? sums[at] : sums[at] + sums[N::SUMS + at];
+            return !N::SPLIT && held ? v * row_most[1][r] + partial[i] * row_most[2][r] : v;
+        };
         const bool complete = whole && last_part;
         if (complete) {
             if (warp == 0 && g == 0) {
@@ -847,21 +876,22 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
                 const int r = i / D, row = (row0 + r) / G, head = now.head * G + (row0 + r) % G;
                 const float by = row_total[0][r];
                 static_cast<T *>(P.y)[(int64_t)(now.q.row + row) * P.y_stride + (int64_t)head * D + i % D] =
-                    narrow<T>(by == 0.0f ? 0.0f : sum_at(r, i % D) * by * row_unit[0][r]);
+                    narrow<T>(by == 0.0f ? 0.0f : sum_at(i) * by * row_unit[0][r]);
             }
         } else {
-            float *const to = P.partial + ((int64_t)worker * 2 + slot) * ROWS * D;
-            for (int i = tid; i < rows * D; i += kThreads) to[i] = sum_at(i / D, i % D);
+            for (int i = tid; i < rows * D; i += kThreads) partial[i] = sum_at(i);
             if (warp == 0 && g == 0) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        P.stats[((int64_t)worker * 2 + slot) * ROWS + 8 * n + 2 * t + j] = make_float4(top[n][j], total[n][j], top_unit[n][j], 0.0f);
+                        stats[8 * n + 2 * t + j] = make_float4(top[n][j], total[n][j], top_unit[n][j], 0.0f);
             }
         }
         __syncthreads();
-        if (todo > 0) {                                    // on to the next tile of rows
+        held = !last_part;
+        if (held) now.unit += units;                       // on with the tile, if there is anything to do
+        else if (todo > 0) {                               // on to the next tile of rows
             now.unit = now.q.units - 1;
             next_place<ROWS>(P, now);
             whole = true;

@@ -175,7 +175,7 @@ struct RunParams {
     struct Cut *cut;                 // [workers]
     int8_t *q_bytes;                 // wide_kernel: [kv_heads][rows * group][terms][dim]: the queries' integers, bytes of the lowest value first
     float *q_factor;                 // [kv_heads][rows * group]: what they are multiples of, times the scale
-    float4 *fold;                    // wide_kernel, fp32: [workers][dim/4][128 rows], where a worker keeps totals that tensor memory has no room for
+    float4 *fold;                    // wide_kernel: [workers][dim/4][128 rows], where a worker keeps totals that tensor memory has no room for
     int workers, early;
     int launched;                    // how many kernels share the sequences: 1 (this one takes all) or 2
     int *status;

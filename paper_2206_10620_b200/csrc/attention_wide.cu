@@ -52,8 +52,9 @@ template <int DT, int D> struct Wide {
     // 1.8e-6 on average, in one direction.  fp32 layers add up FOLD units at a time, and the totals apart: in tensor memory
     // where there is room, else in the workspace.  Root mean square errors, and us for 2 x 1024 rows over 5000 tokens, dim 128: 2.3e-6 and
     // 495 without, 6.9e-7 and 510 by fours, 5.1e-7 and 533 by twos; dim 64 (workspace) 1.4e-6 and 304, 7.0e-7 and 329, 5.0e-7 and 367.
+    // fp16 layers 64: over 262144 tokens as one sum their values were short of two fp16 steps.  (The same sizes, dim 128: 305 without, 307.)
     static constexpr bool FOLD_NEAR = TERMS * kWideUnit + 2 * D <= COLUMNS;
-    static constexpr int FOLD = !SPLIT ? 1 << 30 : FOLD_NEAR ? 2 : 4;
+    static constexpr int FOLD = !SPLIT ? 64 : FOLD_NEAR ? 2 : 4;
     // Sums of two terms lose their lowest bits, so that what is left goes into 23: an error of at most what the query row's largest component
     // times 1/256 (1/128) of a key step gives (fp16 queries would have up to 16 steps' worth in a sum of 128).
     static constexpr int DROP = D <= 128 ? 7 : 8;
@@ -404,7 +405,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         raw[i] = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
                     }
                     if (u > 0) wait(bar_o, phase_o);      // the product before: values, probabilities and sums are free
-                    if (W::SPLIT && u > 0 && u % W::FOLD == 0) {
+                    if (u > 0 && u % W::FOLD == 0) {
 #pragma unroll 1
                         for (int c = 0; c < D / 16; ++c) {
                             uint32_t r[16];
@@ -569,7 +570,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 uint32_t r[16];
                 tmem_ld16(t_sums + my_lanes + c * 16, r);
                 tmem_wait_ld();
-                if (W::SPLIT && units > W::FOLD) add_totals(c, r, since);
+                if (units > W::FOLD) add_totals(c, r, since);
                 if (tid < rows) {
                     float x[16];
 #pragma unroll
@@ -704,7 +705,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kQueryThreads) query_
 template <int DT, int D> static WideKernel wide_of() {
     using W = Wide<DT, D>;
     if constexpr (W::SHARED > 216 * 1024) return {};
-    else return {(const void *)wide_kernel<DT, D>, (const void *)query_kernel<DT, D>, W::SHARED, W::BLOCKS, W::TERMS, W::SPLIT && !W::FOLD_NEAR};
+    else return {(const void *)wide_kernel<DT, D>, (const void *)query_kernel<DT, D>, W::SHARED, W::BLOCKS, W::TERMS, !W::FOLD_NEAR};
 }
 template <int DT> static WideKernel wide_dt(int dim) {
     switch (dim) {
