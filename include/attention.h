@@ -132,6 +132,13 @@ xgen_status xgen_attention_run(const xgen_attention_packed *packed, const void *
  * a kernel's own waits ran out (two seconds; its results are not complete). */
 xgen_status xgen_attention_last_status(const xgen_attention_packed *packed, void *cuda_stream);
 
+/*
+ * Testing aid, not for production use: with extra > 0 the products of every later xgen_attention_run that has many rows wait, 50 ms at
+ * most, for `extra` arrivals (1000 at most) more than will ever come, so that the call ends with XGEN_ERR_TIMEOUT in
+ * xgen_attention_last_status; 0 restores normal operation.  Errors: INVALID_ARG.
+ */
+xgen_status xgen_attention_test_expect_arrivals(xgen_attention_packed *packed, int32_t extra);
+
 /* Release the handle and its device memory.  NULL is allowed. */
 void xgen_attention_free(xgen_attention_packed *packed);
 

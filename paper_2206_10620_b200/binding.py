@@ -34,7 +34,7 @@ EXPORTS = ["xgen_patconv_pack", "xgen_patconv_run", "xgen_patconv_run_static_scr
            "xgen_dwconv_pack", "xgen_dwconv_run", "xgen_dwconv_query", "xgen_dwconv_free",
            "xgen_adapters_pack", "xgen_adapters_run", "xgen_adapters_last_status", "xgen_adapters_free",
            "xgen_attention_pack", "xgen_attention_append", "xgen_attention_read", "xgen_attention_workspace",
-           "xgen_attention_run", "xgen_attention_last_status", "xgen_attention_free",
+           "xgen_attention_run", "xgen_attention_last_status", "xgen_attention_test_expect_arrivals", "xgen_attention_free",
            "xgen_logprobs_pack", "xgen_logprobs_run", "xgen_logprobs_free"]
 
 
@@ -222,6 +222,7 @@ def lib():
         L.xgen_attention_workspace.argtypes = [P, ctypes.POINTER(AttentionBatch), ctypes.POINTER(J)]
         L.xgen_attention_run.argtypes = [P, P, J, ctypes.POINTER(AttentionBatch), ctypes.POINTER(AttentionCache), P, J, P, P]
         L.xgen_attention_last_status.argtypes = [P, P]
+        L.xgen_attention_test_expect_arrivals.argtypes = [P, ctypes.c_int32]
         L.xgen_logprobs_pack.argtypes = [ctypes.POINTER(LogProbsDesc), ctypes.c_int, ctypes.POINTER(P)]
         L.xgen_logprobs_run.argtypes = [P, P, J, J, P, P, P, P, P, P]
         for name in ("adapters", "attention", "logprobs"):
@@ -603,6 +604,9 @@ class Attention(_Handle):
 
     def sync(self, stream=0):
         _check(lib().xgen_attention_last_status(self._h, stream or None), "xgen_attention_last_status")
+
+    def test_expect_arrivals(self, extra):
+        _check(lib().xgen_attention_test_expect_arrivals(self._h, int(extra)), "xgen_attention_test_expect_arrivals")
 
 
 class LogProbs(_Handle):

@@ -28,6 +28,7 @@ struct xgen_attention_packed {
     int wide_workers;           // blocks of wide_kernel, or 0 where there is none
     uint64_t *d_freq;           // [rotary/2] turns per position, as 64-bit fractions; behind them the cosines and sines of the slots of a page
     int *d_status;
+    int extra_arrivals;         // see xgen_attention_test_expect_arrivals
 };
 
 namespace attention {
@@ -1278,6 +1279,7 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     P.group = group; P.window = h->d.window;
     P.scale = (float)((double)h->d.softmax_scale * 1.4426950408889634);
     P.status = h->d_status; P.early = 16;
+    P.extra = h->extra_arrivals; P.limit_us = h->extra_arrivals ? 50000u : 2000000u;
     P.vec_y = (uintptr_t)y % 16 == 0 && y_stride * eb % 16 == 0;
     P.launched = (route.eights ? 1 : 0) + (route.wide ? 1 : 0);
     OnDevice on(h->device);
@@ -1314,6 +1316,12 @@ xgen_status xgen_attention_last_status(const xgen_attention_packed *h, void *str
     if (!h) return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
     return take_status(h->device, h->d_status, 2, stream);
+}
+
+xgen_status xgen_attention_test_expect_arrivals(xgen_attention_packed *h, int32_t extra) {
+    if (!h || extra < 0 || extra > 1000) return XGEN_ERR_INVALID_ARG;
+    h->extra_arrivals = extra;
+    return XGEN_OK;
 }
 
 void xgen_attention_free(xgen_attention_packed *h) {

@@ -177,6 +177,8 @@ struct RunParams {
     float *q_factor;                 // [kv_heads][rows * group]: what they are multiples of, times the scale
     float4 *fold;                    // wide_kernel: [workers][dim/4][128 rows], where a worker keeps totals that tensor memory has no room for
     int workers, early;
+    uint32_t limit_us;               // of wide_kernel's waits
+    int extra;                       // arrivals that its products' barrier waits for in vain (a testing aid)
     int launched;                    // how many kernels share the sequences: 1 (this one takes all) or 2
     int *status;
 };

@@ -99,12 +99,12 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     __shared__ int64_t units_of[kWideSequences];                            // of a key head
     __shared__ int64_t scan[kW + 1], start_units;
     __shared__ int start_s, start_tile, start_unit;
-    __shared__ __align__(8) uint64_t bars[5];
+    __shared__ __align__(8) uint64_t bars[6];
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int H = P.cache.heads, G = P.group, worker = blockIdx.x;
-    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]), bar_p = smem_at(&bars[2]), bar_c = smem_at(&bars[3]);
+    const uint32_t bar_s = smem_at(&bars[0]), bar_o = smem_at(&bars[1]), bar_p = smem_at(&bars[2]), bar_c = smem_at(&bars[3]), bar_end = smem_at(&bars[5]);
     wait_before();
 
     // ---- this block's piece of the line of units: sequences, key heads, tiles, units
@@ -125,10 +125,11 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             scan[0] = 0;
             s_abort = 0;
             mbar_init(bar_s, 1);
-            mbar_init(bar_o, 1);
+            mbar_init(bar_o, 1 + P.extra);
             mbar_init(bar_p, kWideRows);
             mbar_init(bar_c, 32);
             mbar_init(bar_c + 8, 32);
+            mbar_init(bar_end, 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncthreads();
@@ -208,12 +209,14 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     tc_fence_after();
     const uint32_t tmem = s_tmem, my_lanes = (uint32_t)(warp * 32) << 16, t_scores = tmem, t_sums = tmem + TERMS * kWideUnit;
     int *const timeout = P.status + 1;
-    const auto wait = [&](uint32_t bar, int &phase) {
-        mbar_wait<false>(bar, (uint32_t)(phase & 1), &s_abort, timeout, 2000000u);
-        ++phase;
-        __syncwarp();
+    // Whether it came, the same for the whole warp.  A warp whose wait runs out copies, issues and writes no more: so do the others' waits for it,
+    // soon after, and the block ends once the matrix instructions that are under way have.
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+        const bool came = __all_sync(~0u, mbar_wait<false>(bar, parity, &s_abort, timeout, P.limit_us));
         tc_fence_after();
+        return came;
     };
+    bool stop = false;
     int phase_s = 0, phase_o = 0, phase_p = 0, phase_c = 0;      // (phase_c counts steps: two barriers in turn)
     constexpr uint32_t IDESC_S = ((uint32_t)(kWideUnit >> 3) << 17) | (8u << 24) | (2u << 4) | (1u << 7) | (1u << 10);      // s8 s8 -> s32
     constexpr uint32_t IDESC_O = ((uint32_t)(D >> 3) << 17) | (8u << 24) | (1u << 4) | (1u << 16);                          // f16 f16 (transposed) -> f32
@@ -316,10 +319,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                     fence_async_proxy();
                     patconv::mbar_arrive(bar_c + 8 * stage);
                 }
-                mbar_wait<false>(bar_p, (uint32_t)(phase_p & 1), &s_abort, timeout, 2000000u);
-                ++phase_p;
-                __syncwarp();
-                tc_fence_after();
+                if (!wait(bar_p, phase_p++ & 1)) { stop = true; break; }
                 if (lane == 0) {
                     if (u >= 0) {
 #pragma unroll
@@ -370,8 +370,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
 #pragma unroll 1
             for (int u = 0; u < units; ++u) {
                 const int stage = phase_c & 1, token = token_begin + u * kWideUnit;
-                mbar_wait<false>(bar_c + 8 * stage, (uint32_t)(phase_c >> 1 & 1), &s_abort, timeout, 2000000u);
-                ++phase_c;
+                if (!wait(bar_c + 8 * stage, phase_c++ >> 1 & 1)) { stop = true; break; }
                 const unsigned there = stage_there[stage] & 15u, lost = stage_there[stage] >> 4;
                 float k_scale[4];
 #pragma unroll
@@ -404,7 +403,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                         const int p = tid + kWideRows * i, block = (p >> 3) / CHUNKS, c = (p >> 3) % CHUNKS;
                         raw[i] = *reinterpret_cast<const uint4 *>(from + block * (D * 8) + c * 128 + (p & 7) * 16);
                     }
-                    if (u > 0) wait(bar_o, phase_o);      // the product before: values, probabilities and sums are free
+                    if (u > 0 && !wait(bar_o, phase_o++ & 1)) { stop = true; break; }       // the product before: values, probabilities and sums are free
                     if (u > 0 && u % W::FOLD == 0) {
 #pragma unroll 1
                         for (int c = 0; c < D / 16; ++c) {
@@ -428,7 +427,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                     }
                 }
                 // ---- scores in powers of two
-                wait(bar_s, phase_s);
+                if (!wait(bar_s, phase_s++ & 1)) { stop = true; break; }
                 float sc[kWideUnit];
                 constexpr int TOGETHER = TERMS == 3 ? 1 : 2;      // (loads are waited for all at once)
                 uint32_t rr[TOGETHER][TERMS][16];
@@ -555,11 +554,11 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 }
                 hand_over();
             }
-            wait(bar_o, phase_o);
+            if (!stop) stop = !wait(bar_o, phase_o++ & 1);
         }
         todo -= units;
 
-        if (warp < kRowWarps) {
+        if (warp < kRowWarps && !stop) {
             // ---- the tile's results: a row to a thread
             const bool complete = whole && last_part;
             const float2 f = complete ? result_factors(l, unit) : make_float2(1.0f, 1.0f);
@@ -598,8 +597,9 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
             if (!complete) P.stats[((int64_t)worker * 2 + slot) * kWideRows + tid] = make_float4(m, l, unit, 0.0f);
         }
         tc_fence_before();
-        __syncthreads();
+        stop = __syncthreads_or(stop);
         tc_fence_after();
+        if (stop) break;
         if (todo > 0) {
             skipped = 0;
             if (++tile >= q.tiles) {
@@ -615,6 +615,11 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
     }
     let_next();
     copy_async_wait<0>();
+    if (stop && warp == kRowWarps) {
+        if (lane == 0) tc_commit<false>(bar_end, 0);
+        __syncwarp();
+        wait(bar_end, 0);
+    }
     tc_fence_before();
     __syncthreads();
     if (warp == kRowWarps) tmem_free<false>(tmem, W::COLUMNS);
