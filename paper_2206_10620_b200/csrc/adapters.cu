@@ -281,7 +281,7 @@ template <int DT, int RP, int ROWS> __global__ void __launch_bounds__(ROWS == 64
             const int at = b * BLOCK + t * E;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                f.u[i] = in[i] && P.vec_x && at + E <= P.k ? __ldg(reinterpret_cast<const uint4 *>(x + (row0 + 8 * i + g) * P.x_stride + at)) : part_of_row(i, at);
+                f.u[i] = in[i] && P.vec_x && at + E <= P.k ? *reinterpret_cast<const uint4 *>(x + (row0 + 8 * i + g) * P.x_stride + at) : part_of_row(i, at);
 #pragma unroll
             for (int j = 0; j < NT; ++j) f.w[j] = __ldg(w + ((int64_t)b * NT + j) * 32);
         };

@@ -121,8 +121,8 @@ template <int DT, int LAY, int ITEMS> __device__ __forceinline__ void append_hea
             const bool there = token0 + i * step < part.n;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                raw[i][w] = there ? __ldg(reinterpret_cast<const uint4 *>(from + at0) + w) : make_uint4(0, 0, 0, 0);
-                raw[i][W + w] = there ? __ldg(reinterpret_cast<const uint4 *>(from + at1) + w) : make_uint4(0, 0, 0, 0);
+                raw[i][w] = there ? reinterpret_cast<const uint4 *>(from + at0)[w] : make_uint4(0, 0, 0, 0);
+                raw[i][W + w] = there ? reinterpret_cast<const uint4 *>(from + at1)[w] : make_uint4(0, 0, 0, 0);
             }
         }
     };

@@ -76,7 +76,7 @@ template <int DT> struct Piece {
     static constexpr int VEC = 16 / sizeof(T);
     uint32_t u[4];
     __device__ __forceinline__ void load(const T *p) {
-        take(__ldg(reinterpret_cast<const uint4 *>(p)));
+        take(*reinterpret_cast<const uint4 *>(p));
     }
     __device__ __forceinline__ void take(const uint4 &r) {
         u[0] = r.x; u[1] = r.y; u[2] = r.z; u[3] = r.w;

@@ -25,7 +25,8 @@ struct OnDevice {
 };
 
 // One launch on the caller's stream.  The kernel may start while its predecessor ends: it calls wait_before() ahead of its
-// first access to memory that the predecessor could write or still read.  cluster: blocks along x that form one, or 1.
+// first access to memory that the predecessor could write or still read, and reads none of it by read-only loads (__ldg): those are for
+// what nobody writes while the kernel lives, and it lives while its predecessor writes.  cluster: blocks along x that form one, or 1.
 inline xgen_status launch(const void *kern, dim3 grid, dim3 block, size_t shared, void *stream, void **args, int cluster = 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = shared; cfg.stream = (cudaStream_t)stream;
