@@ -97,7 +97,8 @@ xgen_status xgen_attention_pack(const xgen_attention_desc *desc, const double *f
  * Write the batch's new keys and values into the cache.
  *   k_dev, v_dev  [rows] rows of kv_heads * head_dim elements, kv_stride elements apart (both may be parts of one
  *                 product's rows), element-aligned, outside the cache
- * Only enqueues one kernel.  Errors: INVALID_ARG (null or misaligned pointer), SHAPE, CUDA.
+ * Only enqueues one kernel.  Errors: INVALID_ARG (null or misaligned pointer; keys, values or what describes the batch in the cache, or its
+ * parts over each other), SHAPE, CUDA.
  */
 xgen_status xgen_attention_append(const xgen_attention_packed *packed, const void *k_dev, const void *v_dev, int64_t kv_stride,
                                   const xgen_attention_batch *batch, const xgen_attention_cache *cache, void *cuda_stream);
@@ -105,7 +106,8 @@ xgen_status xgen_attention_append(const xgen_attention_packed *packed, const voi
 /*
  * Give back what the cache holds of the batch's rows (to hand a prefix on, to check): codes times scales, keys turned.
  *   out_dtype            XGEN_F32 or XGEN_F16_F32ACC, whatever the handle's type
- *   k_out_dev, v_out_dev [rows] rows of kv_heads * head_dim elements, out_stride apart, element-aligned
+ *   k_out_dev, v_out_dev [rows] rows of kv_heads * head_dim elements, out_stride apart, element-aligned, outside the cache and what describes
+ *                        the batch; no element of one is one of the other's (they may be parts of the same rows)
  * Only enqueues one kernel.  Errors as for append, and UNSUPPORTED (out_dtype).
  */
 xgen_status xgen_attention_read(const xgen_attention_packed *packed, const xgen_attention_batch *batch, const xgen_attention_cache *cache,
@@ -118,8 +120,8 @@ xgen_status xgen_attention_workspace(const xgen_attention_packed *packed, const 
 /*
  * Attention of the batch's rows over the cache (which holds them already: append first).
  *   q_dev  [rows] rows of q_heads * head_dim elements, q_stride apart, element-aligned
- *   y_dev  [rows] rows likewise, y_stride apart, outside q_dev
- *   workspace_dev  xgen_attention_workspace bytes, 16-byte aligned.  Nothing in it counts between calls; calls that
+ *   y_dev  [rows] rows likewise, y_stride apart, outside q_dev, the cache and what describes the batch
+ *   workspace_dev  xgen_attention_workspace bytes, 16-byte aligned, outside all of these.  Nothing in it counts between calls; calls that
  *          may run at the same time need one each
  * Only enqueues kernels: two for a few rows of each sequence, three more where a sequence may have many.
  * Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (rows times q_heads / kv_heads above 2^31 too), CUDA.

@@ -1057,6 +1057,28 @@ static bool in_cache(const xgen_attention_packed &h, const xgen_attention_cache 
     const size_t scales = (size_t)c.pages * h.d.kv_heads * 4, codes = (size_t)c.pages * h.d.kv_heads * h.d.page_tokens * h.d.head_dim;
     return overlap(p, n, c.k_codes_dev, codes) || overlap(p, n, c.v_codes_dev, codes) || overlap(p, n, c.k_scale_dev, scales) || overlap(p, n, c.v_scale_dev, scales);
 }
+// Whether the bytes meet what describes the batch.
+static bool in_batch(const xgen_attention_batch &b, const void *p, size_t n) {
+    const size_t s = (size_t)b.sequences;
+    return overlap(p, n, b.row_start_dev, (s + 1) * 4) || overlap(p, n, b.length_dev, s * 4) || overlap(p, n, b.page_table_dev, s * (size_t)b.table_stride * 4);
+}
+// Whether the parts of a cache meet each other, or the batch.
+static bool cache_is_apart(const xgen_attention_packed &h, const xgen_attention_batch &b, const xgen_attention_cache &c) {
+    const size_t scales = (size_t)c.pages * h.d.kv_heads * 4, codes = (size_t)c.pages * h.d.kv_heads * h.d.page_tokens * h.d.head_dim;
+    const struct { const void *p; size_t n; } part[] = {{c.k_codes_dev, codes}, {c.v_codes_dev, codes}, {c.k_scale_dev, scales}, {c.v_scale_dev, scales}};
+    for (int i = 0; i < 4; ++i) {
+        if (in_batch(b, part[i].p, part[i].n)) return false;
+        for (int o = 0; o < i; ++o)
+            if (overlap(part[i].p, part[i].n, part[o].p, part[o].n)) return false;
+    }
+    return true;
+}
+// Whether two sets of rows of `width` bytes, `stride` apart in both, share a byte: those of one may lie between those of the other.
+static bool rows_meet(const void *a, const void *b, int64_t rows, size_t stride, size_t width) {
+    const size_t d = (uintptr_t)a < (uintptr_t)b ? (uintptr_t)b - (uintptr_t)a : (uintptr_t)a - (uintptr_t)b;
+    const size_t n = d / stride, rest = d % stride;                    // row 0 of the later one begins in row n of the other, or behind it
+    return (n < (size_t)rows && rest < width) || (n + 1 < (size_t)rows && stride - rest < width);
+}
 // Pages that the batch's rows reach, at most: n tokens of a sequence reach (n - 1)/page_tokens + 2 of them, and not more than n.
 static int64_t pages_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
     const int64_t pages = b.rows / h.d.page_tokens + 2 * (int64_t)b.sequences;
@@ -1196,7 +1218,7 @@ xgen_status xgen_attention_append(const xgen_attention_packed *h, const void *k,
     if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
     if (!k || !v) return XGEN_ERR_INVALID_ARG;
     const size_t eb = element_bytes(h->d.dtype), bytes = span_bytes(b->rows, stride, width, eb);
-    if (((uintptr_t)k | (uintptr_t)v) % eb || in_cache(*h, *c, k, bytes) || in_cache(*h, *c, v, bytes)) return XGEN_ERR_INVALID_ARG;
+    if (((uintptr_t)k | (uintptr_t)v) % eb || in_cache(*h, *c, k, bytes) || in_cache(*h, *c, v, bytes) || !cache_is_apart(*h, *b, *c)) return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
     AppendParams P{};
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
@@ -1230,7 +1252,9 @@ xgen_status xgen_attention_read(const xgen_attention_packed *h, const xgen_atten
     if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
     if (!k || !v) return XGEN_ERR_INVALID_ARG;
     const size_t eb = element_bytes(out_dtype), bytes = span_bytes(b->rows, stride, width, eb);
-    if (((uintptr_t)k | (uintptr_t)v) % eb || in_cache(*h, *c, k, bytes) || in_cache(*h, *c, v, bytes)) return XGEN_ERR_INVALID_ARG;
+    if (((uintptr_t)k | (uintptr_t)v) % eb || in_cache(*h, *c, k, bytes) || in_cache(*h, *c, v, bytes) || in_batch(*b, k, bytes) || in_batch(*b, v, bytes) ||
+        rows_meet(k, v, b->rows, stride * eb, width * eb))
+        return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
     ReadParams P{};
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c);
@@ -1266,12 +1290,15 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     if (q_stride < width || y_stride < width || q_stride > (1ll << 31) || y_stride > (1ll << 31) || b->rows * group > INT32_MAX - 64) return XGEN_ERR_SHAPE;
     if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
     if (!q || !y || !workspace) return XGEN_ERR_INVALID_ARG;
-    const size_t eb = element_bytes(h->d.dtype), y_bytes = span_bytes(b->rows, y_stride, width, eb);
-    if (((uintptr_t)q | (uintptr_t)y) % eb || (uintptr_t)workspace % 16 || overlap(y, y_bytes, q, span_bytes(b->rows, q_stride, width, eb)) ||
-        in_cache(*h, *c, y, y_bytes))
+    const size_t eb = element_bytes(h->d.dtype), y_bytes = span_bytes(b->rows, y_stride, width, eb), q_bytes = span_bytes(b->rows, q_stride, width, eb);
+    if (((uintptr_t)q | (uintptr_t)y) % eb || (uintptr_t)workspace % 16 || overlap(y, y_bytes, q, q_bytes) ||
+        in_cache(*h, *c, y, y_bytes) || in_batch(*b, y, y_bytes))
         return XGEN_ERR_INVALID_ARG;
     if (h->device < 0) return XGEN_ERR_CUDA;
-    if (overlap(workspace, workspace_of(*h, *b), y, y_bytes) || in_cache(*h, *c, workspace, workspace_of(*h, *b))) return XGEN_ERR_INVALID_ARG;
+    const size_t work_bytes = (size_t)workspace_of(*h, *b);
+    if (overlap(workspace, work_bytes, y, y_bytes) || overlap(workspace, work_bytes, q, q_bytes) || in_cache(*h, *c, workspace, work_bytes) ||
+        in_batch(*b, workspace, work_bytes))
+        return XGEN_ERR_INVALID_ARG;
     const Route route = route_of(*h, *b);
     RunParams P{};
     P.batch = batch_of(*b); P.cache = cache_of(*h, *c); P.rotation = rotation_of(*h);
