@@ -60,7 +60,7 @@ xgen_status xgen_adapters_pack(const xgen_adapters_desc *desc, const void *a_hos
  * counts as none and, where its request has rows, is reported by xgen_adapters_last_status.
  * Only enqueues one kernel on the stream, on the handle's device; no workspace.  rows = 0 or requests = 0 does nothing.
  * Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (negative sizes, a stride below the
- * row's length, rows or requests above 2^31-1, too many of both for one launch), CUDA.
+ * row's length or above 2^31, rows or requests above 2^31-1, too many of both for one launch), CUDA.
  */
 xgen_status xgen_adapters_run(const xgen_adapters_packed *packed, const void *x_dev, int64_t rows, int64_t x_stride,
                               const int32_t *row_start_dev, const int32_t *adapter_dev, int64_t requests, const void *y_dev,

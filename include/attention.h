@@ -5,7 +5,7 @@
  * A batch is a number of sequences.  Sequence i has length[i] tokens so far, of which the last ones are new in
  * this call: the rows row_start[i] .. row_start[i+1]-1 of the new keys, values or queries, at the positions length[i] - n
  * .. length[i] - 1.  (Rows whose position would be negative are neither appended nor read back, and see nothing as queries.)
- * Lengths are at most 2^30.
+ * Lengths are at most 2^30, rows at most 2^31 elements apart.
  *
  * The cache is a set of pages.  A page holds, for every key/value head, page_tokens tokens of head_dim signed
  * 8-bit codes, and one fp32 scale for the keys and one for the values: a code c stands for c * scale.

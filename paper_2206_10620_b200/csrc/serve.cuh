@@ -44,10 +44,10 @@ inline xgen_status launch(const void *kern, dim3 grid, dim3 block, size_t shared
     return XGEN_OK;
 }
 
-// Whether [a, a + an) and [b, b + bn) share a byte.
+// Whether [a, a + an) and [b, b + bn) share a byte (of addresses that do not end: a span may be longer than what is left of them).
 inline bool overlap(const void *a, size_t an, const void *b, size_t bn) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && an && bn && x < y + bn && y < x + an;
+    return a && b && an && bn && (x < y ? y - x < an : x - y < bn);
 }
 
 // The stream's work done, whether the kernels left a mark at `mark` (marks[0]: an argument that does not fit; marks[1], where there are two: a

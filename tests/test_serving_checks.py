@@ -5,7 +5,7 @@ import ctypes
 from paper_2206_10620_b200 import binding
 from test_host_failures import _run, fake_lib  # noqa: F401  (the fixture)
 from test_serving_host_failures import MAKE
-from test_serving_refusals import A, CUDA, INVALID, attention, batch, cache, calls, refused
+from test_serving_refusals import A, CUDA, INVALID, SHAPE, adapters, attention, batch, cache, calls, logprobs, refused
 
 
 def test_a_wait_cannot_be_told_to_expect_fewer_arrivals():
@@ -75,3 +75,20 @@ for first, n in ((10 * Z, 100 * 1024), (2 * Z, 12), (3 * Z, 8), (4 * Z, 72), (11
         assert run(w=w // 16 * 16) == 1, (first, w)
     assert run(w=first + (n + 15) // 16 * 16) == 0 and run(w=(first - size) // 16 * 16) == 0
 """)
+
+
+# --- sizes ----------------------------------------------------------------------------------------------
+ROWS, STRIDE = (1 << 31) - 1, 1 << 31                       # fp32: all but 2^34 of the 2^64 bytes that addresses reach
+
+
+def test_spans_that_reach_past_the_last_address_overlap_what_is_behind_them():
+    op = adapters()
+    good = dict(x_ptr=A, rows=4, x_stride=8, row_start_ptr=2 * A, adapter_ptr=3 * A, requests=2, y_ptr=4 * A, y_stride=8, out_ptr=5 * A, out_stride=8)
+    far = 1 << 36
+    refused(INVALID, op.run, **{**good, "rows": ROWS, "x_stride": STRIDE, "x_ptr": far, "out_ptr": 1 << 45, "y_ptr": 1 << 50})
+    refused(INVALID, op.run, **{**good, "rows": ROWS, "y_ptr": far, "y_stride": STRIDE, "x_ptr": 1 << 58, "out_ptr": 1 << 45})
+    refused(INVALID, op.run, **{**good, "rows": ROWS, "out_ptr": far, "out_stride": STRIDE, "y_ptr": 1 << 45})
+    _, read, run = calls(attention(q=1, kv=1))
+    near = cache(1 << 30, 1 << 31, 1 << 32, 1 << 33)
+    refused(INVALID, run, b=batch(rows=ROWS - 64), q=far, q_stride=STRIDE, c=near, y=1 << 45)
+    refused(INVALID, read, b=batch(rows=ROWS), stride=STRIDE, k=far, v=far + (1 << 30), c=cache(1 << 30, 1 << 31, 1 << 32, 1 << 60))
