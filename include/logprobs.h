@@ -51,8 +51,8 @@ xgen_status xgen_logprobs_pack(const xgen_logprobs_desc *desc, int device, xgen_
  *   top_logprob_dev [rows][top] fp32; likewise
  * Outputs must overlap neither the inputs nor each other.  Only enqueues one kernel on the stream, on the handle's
  * device; no workspace.  rows = 0 does nothing.
- * Errors: INVALID_ARG (null or misaligned pointer, overlap, nothing asked for), SHAPE (rows < 0 or above 2^31-1, a stride below vocab, a
- * tensor beyond 2^62 bytes), CUDA.
+ * Errors: INVALID_ARG (null or misaligned pointer, overlap, nothing asked for), SHAPE (rows < 0 or above 2^31-1, a stride below vocab or above 2^31,
+ * logits beyond 2^62 bytes), CUDA.
  */
 xgen_status xgen_logprobs_run(const xgen_logprobs_packed *packed, const void *x_dev, int64_t rows, int64_t row_stride,
                               const int32_t *token_dev, float *logprob_dev, float *entropy_dev, int32_t *top_dev,

@@ -531,12 +531,13 @@ xgen_status xgen_logprobs_run(const xgen_logprobs_packed *h, const void *x, int6
                               float *logprob, float *entropy, int32_t *top, float *top_logprob, void *stream) {
     if (!h) return XGEN_ERR_INVALID_ARG;
     if (rows < 0 || rows > INT32_MAX || stride < h->d.vocab || stride > (1ll << 31)) return XGEN_ERR_SHAPE;
+    const size_t eb = element_bytes(h->d.dtype);
+    if (rows && ((size_t)(rows - 1) * stride + h->d.vocab) * eb > (size_t)1 << 62) return XGEN_ERR_SHAPE;       // (2^64 - 2^33 at most)
     if ((logprob != nullptr) != (token != nullptr) || (top != nullptr) != (h->d.top > 0) || (top_logprob != nullptr) != (h->d.top > 0))
         return XGEN_ERR_INVALID_ARG;
     if (!logprob && !entropy && !top) return XGEN_ERR_INVALID_ARG;
     if (rows == 0) return XGEN_OK;
     if (!x) return XGEN_ERR_INVALID_ARG;
-    const size_t eb = element_bytes(h->d.dtype);
     if ((uintptr_t)x % eb || ((uintptr_t)token | (uintptr_t)logprob | (uintptr_t)entropy | (uintptr_t)top | (uintptr_t)top_logprob) % 4)
         return XGEN_ERR_INVALID_ARG;
     {

@@ -92,3 +92,13 @@ def test_spans_that_reach_past_the_last_address_overlap_what_is_behind_them():
     near = cache(1 << 30, 1 << 31, 1 << 32, 1 << 33)
     refused(INVALID, run, b=batch(rows=ROWS - 64), q=far, q_stride=STRIDE, c=near, y=1 << 45)
     refused(INVALID, read, b=batch(rows=ROWS), stride=STRIDE, k=far, v=far + (1 << 30), c=cache(1 << 30, 1 << 31, 1 << 32, 1 << 60))
+
+
+def test_logits_of_more_bytes_than_there_are():
+    op = logprobs()
+    run = lambda rows, **kw: op.run(**{**dict(x_ptr=8 * A, rows=rows, row_stride=STRIDE, token_ptr=2 * A, logprob_ptr=0, entropy_ptr=4 * A,      # noqa: E731
+                                              top_ptr=5 * A, top_logprob_ptr=6 * A), **kw})
+    refused(SHAPE, run, ROWS, token_ptr=0)
+    refused(SHAPE, run, (1 << 29) + 1, token_ptr=0)         # 2^62 + 40
+    refused(CUDA, run, 4, token_ptr=0)
+    refused(INVALID, run, 1 << 29, token_ptr=0, entropy_ptr=1 << 50)
