@@ -528,8 +528,9 @@ xgen_status xgen_adapters_pack(const xgen_adapters_desc *d, const void *a, const
     const size_t eb = element_bytes(d->dtype);
     const int rp = d->rank <= 16 ? 16 : d->rank <= 32 ? 32 : d->rank <= 64 ? 64 : 128;
     const int kp = (d->k + 31) / 32 * 32, np = (d->c_out + 31) / 32 * 32;
-    const size_t na = (size_t)d->adapters * rp * kp * eb, nb = (size_t)d->adapters * rp * np * eb;
-    if (na + nb > (size_t)1 << 40) return XGEN_ERR_SHAPE;
+    const size_t one_a = (size_t)rp * kp * eb, one_b = (size_t)rp * np * eb;       // (2^33 at most)
+    if ((size_t)d->adapters > ((size_t)1 << 40) / (one_a + one_b)) return XGEN_ERR_SHAPE;
+    const size_t na = d->adapters * one_a, nb = d->adapters * one_b;
     xgen_adapters_packed *h = new (std::nothrow) xgen_adapters_packed();
     if (!h) return XGEN_ERR_ALLOC;
     h->d = *d; h->device = device; h->rp = rp; h->kp = kp; h->np = np;

@@ -102,3 +102,16 @@ def test_logits_of_more_bytes_than_there_are():
     refused(SHAPE, run, (1 << 29) + 1, token_ptr=0)         # 2^62 + 40
     refused(CUDA, run, 4, token_ptr=0)
     refused(INVALID, run, 1 << 29, token_ptr=0, entropy_ptr=1 << 50)
+
+
+def test_adapters_of_more_bytes_than_a_number_holds():
+    """2^30 adapters of 2^33 bytes on either side: 2^64 in all."""
+    desc = binding.AdaptersDesc(1 << 24, 1 << 24, 128, 1 << 30, binding.F32)
+    h = ctypes.c_void_p()
+    pack = lambda: binding.lib().xgen_adapters_pack(ctypes.byref(desc), A, A, A, -1, ctypes.byref(h))      # noqa: E731  (nothing reads them)
+    assert pack() == SHAPE and not h
+    desc.adapters = (1 << 31) - 1
+    assert pack() == SHAPE and not h
+    desc.adapters = 64                                      # 2^40 in all
+    assert pack() == 0 and h
+    binding.lib().xgen_adapters_free(h)
