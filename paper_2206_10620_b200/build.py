@@ -31,8 +31,8 @@ _INCLUDES = {
     "dwconv.cu": ["patconv_internal.h", os.path.join(_INC, "patconv.h"), os.path.join(_INC, "dwconv.h")],
     "probe.cu": [os.path.join(_INC, "patconv.h")],
     "pack.cpp": ["patconv_internal.h", os.path.join(_INC, "patconv.h")],
-    **{name + ".cu": ["patconv_internal.h", "serve.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, name + ".h")]
-       for name in ("adapters", "logprobs")},
+    "adapters.cu": ["patconv_internal.h", "ptx.cuh", "serve.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, "adapters.h")],
+    "logprobs.cu": ["patconv_internal.h", "serve.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, "logprobs.h")],
     **{name + ".cu": ["patconv_internal.h", "ptx.cuh", "serve.cuh", "attention.cuh", os.path.join(_INC, "patconv.h"), os.path.join(_INC, "attention.h")]
        for name in ("attention", "attention_wide")},
 }
