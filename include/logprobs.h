@@ -14,7 +14,8 @@
  * A row of nothing but -infinity has an entropy of 0 and log probabilities of -infinity.  A row that holds a
  * NaN or +infinity has NaN everywhere and -1 in top.
  *
- * The row is read once; sums are fp32 (relative error of a sum about 1e-6 at most), logarithms and results fp32.
+ * The row is read once; sums are fp32 (relative error of a sum about 1e-6 at most), logarithms and results fp32: off by some 1e-6, too,
+ * where they are near 0.  No log probability is above 0, no entropy below.
  * Same conventions as patconv.h: plain C ABI, every function returns a status.
  */
 #ifndef XGEN_LOGPROBS_H

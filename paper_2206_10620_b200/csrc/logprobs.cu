@@ -2,8 +2,9 @@
 //
 // One pass over the row: a thread takes every 256th 16-byte piece of its block's part and keeps a reference m near the largest logit
 // so far (raised, and the sums rescaled, only where a logit lies 8 above it: e^8 is no strain on a sum), s = sum e^(x - m) and
-// w = sum e^(x - m) (x - m).  Then lse = m + log s and the entropy is log s - w / s, with no difference of large numbers.  A row goes to a cluster of 1 to 16 blocks, so that a few rows fill
-// the GPU too; what the blocks found meets in shared memory.
+// w = sum e^(x - m) (x - m).  Then lse = m + log s and the entropy is log s - w / s.  m may lie 8 below the largest logit, so where one
+// token has nearly all of the probability these are differences of numbers of up to 8, off by some 1e-6, and held to their sign.  A row
+// goes to a cluster of 1 to 16 blocks, so that a few rows fill the GPU too; what the blocks found meets in shared memory.
 // (What follows the pass over the row is short code, loops not unrolled and sums joined by one function that is called: most of it is
 // run once, and while the GPU reads its rows a line of instructions that no cache holds takes a microsecond to come.)
 //
@@ -448,9 +449,9 @@ template <int DT, bool ENTROPY> __global__ void __launch_bounds__(kThreads, 4) l
         const bool bad = isnan(r.s) || r.m == INFINITY;
         const bool empty = !bad && r.m == -INFINITY;
         const float log_s = logf(r.s);
-        auto answer = [&](float v) { return bad ? NAN : empty ? -INFINITY : (v - r.m) - log_s; };
+        auto answer = [&](float v) { return bad ? NAN : empty ? -INFINITY : fminf((v - r.m) - log_s, 0.0f); };
         if (tid == 0 && P.logprob) P.logprob[row] = token == -1 ? 0.0f : token < 0 || token >= V ? NAN : answer(token_logit);
-        if (ENTROPY && tid == 32) P.entropy[row] = bad ? NAN : empty ? 0.0f : log_s - r.w / r.s;
+        if (ENTROPY && tid == 32) P.entropy[row] = bad ? NAN : empty ? 0.0f : fmaxf(log_s - r.w / r.s, 0.0f);
         auto put = [&](int rank, uint64_t k) {
             P.top_index[row * top + rank] = bad || k == kNone ? -1 : (int)~(uint32_t)k;
             P.top_logprob[row * top + rank] = bad ? NAN : k == kNone ? -INFINITY : answer(unordered((uint32_t)(k >> 32)));
