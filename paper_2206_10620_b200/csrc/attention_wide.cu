@@ -308,6 +308,7 @@ template <int DT, int D> __global__ void __launch_bounds__(kWideThreads, Wide<DT
                 if (u + 1 < units) {                      // the next step's codes are there
                     if (u < 0) copy_async_wait<1>(); else copy_async_wait<0>();
                     const int stage = (phase_c + u + 1) & 1;
+                    __syncwarp();                         // (lane 0 wrote it)
                     const unsigned there = stage_there[stage];
                     const float v = lane < 4 && there >> lane & 1 ? stage_scale[stage][1][lane] : 0.0f;      // (what this lane copied itself)
                     const unsigned lost = __ballot_sync(~0u, !(v < INFINITY));
