@@ -124,7 +124,7 @@ xgen_status xgen_attention_workspace(const xgen_attention_packed *packed, const 
  *   workspace_dev  xgen_attention_workspace bytes, 16-byte aligned, outside all of these.  Nothing in it counts between calls; calls that
  *          may run at the same time need one each
  * Only enqueues kernels: two for a few rows of each sequence, three more where a sequence may have many.
- * Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (rows times q_heads / kv_heads above 2^31 too), CUDA.
+ * Errors: INVALID_ARG (null or misaligned pointer, overlap), SHAPE (rows times q_heads / kv_heads above 2^31 - 257 too), CUDA.
  */
 xgen_status xgen_attention_run(const xgen_attention_packed *packed, const void *q_dev, int64_t q_stride, const xgen_attention_batch *batch,
                                const xgen_attention_cache *cache, void *y_dev, int64_t y_stride, void *workspace_dev, void *cuda_stream);

@@ -377,7 +377,7 @@ template <int ROWS> __device__ __forceinline__ Sequence sequence_of(const RunPar
     q.length = length_of(P.batch, s);
     const int end = (int)min((int64_t)q.length, held);
     if (end < q.length && q.n > 0) atomicExch(P.status, 1);
-    const int first = q.length - q.n;                     // the first row's position (may be negative)
+    const int first = max(q.length - q.n, 0);             // the first row's position, if it has one
     q.from = P.window > 0 && first - P.window + 1 > 0 ? (first - P.window + 1) / kTokens * kTokens : 0;
     if (P.launched > 1 && q.n * P.group > kNarrowMost) q.n = 0;        // another kernel's
     q.tiles = (int)(((int64_t)q.n * P.group + ROWS - 1) / ROWS);
@@ -522,7 +522,7 @@ template <int DT, int D, int NT> __global__ void __launch_bounds__(kThreads, Nar
     auto set_seen = [&] {
         const int before = ahead.q.length - ahead.q.n;     // the first row's position
         last_seen = min(ahead.q.length - 1, before + (ahead.tile * ROWS + ROWS - 1) / G);
-        first_seen = P.window > 0 ? before + ahead.tile * ROWS / G - P.window + 1 : 0;
+        first_seen = P.window > 0 ? max(before + ahead.tile * ROWS / G, 0) - P.window + 1 : 0;
     };
     set_seen();
     // this lane's 16-byte pieces of a tile: row (lane + 32 i) / (D/16), column the rest
@@ -1287,7 +1287,7 @@ xgen_status xgen_attention_run(const xgen_attention_packed *h, const void *q, in
     if (st != XGEN_OK) return st;
     const int64_t width = (int64_t)h->d.q_heads * h->d.head_dim;
     const int group = h->d.q_heads / h->d.kv_heads;
-    if (q_stride < width || y_stride < width || q_stride > (1ll << 31) || y_stride > (1ll << 31) || b->rows * group > INT32_MAX - 64) return XGEN_ERR_SHAPE;
+    if (q_stride < width || y_stride < width || q_stride > (1ll << 31) || y_stride > (1ll << 31) || b->rows * group > INT32_MAX - 256) return XGEN_ERR_SHAPE;
     if (b->sequences == 0 || b->rows == 0) return XGEN_OK;
     if (!q || !y || !workspace) return XGEN_ERR_INVALID_ARG;
     const size_t eb = element_bytes(h->d.dtype), y_bytes = span_bytes(b->rows, y_stride, width, eb), q_bytes = span_bytes(b->rows, q_stride, width, eb);

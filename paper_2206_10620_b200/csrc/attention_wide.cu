@@ -78,7 +78,7 @@ __device__ __forceinline__ WideSequence wide_sequence(const RunParams &P, int s)
 __device__ __forceinline__ WideTile wide_tile(const RunParams &P, const WideSequence &q, int tile) {
     const int before = q.length - q.n, row0 = tile * kWideRows, row1 = min(q.n * P.group, row0 + kWideRows) - 1;
     WideTile t;
-    t.from = P.window > 0 ? max(before + row0 / P.group - P.window + 1, 0) & ~15 : 0;
+    t.from = P.window > 0 ? max(max(before + row0 / P.group, 0) - P.window + 1, 0) & ~15 : 0;
     t.to = max(min(before + row1 / P.group + 1, q.end), t.from);
     t.units = max((t.to - t.from + kWideUnit - 1) / kWideUnit, 1);
     return t;

@@ -90,7 +90,7 @@ def test_spans_that_reach_past_the_last_address_overlap_what_is_behind_them():
     refused(INVALID, op.run, **{**good, "rows": ROWS, "out_ptr": far, "out_stride": STRIDE, "y_ptr": 1 << 45})
     _, read, run = calls(attention(q=1, kv=1))
     near = cache(1 << 30, 1 << 31, 1 << 32, 1 << 33)
-    refused(INVALID, run, b=batch(rows=ROWS - 64), q=far, q_stride=STRIDE, c=near, y=1 << 45)
+    refused(INVALID, run, b=batch(rows=ROWS - 256), q=far, q_stride=STRIDE, c=near, y=1 << 45)
     refused(INVALID, read, b=batch(rows=ROWS), stride=STRIDE, k=far, v=far + (1 << 30), c=cache(1 << 30, 1 << 31, 1 << 32, 1 << 60))
 
 
@@ -115,3 +115,11 @@ def test_adapters_of_more_bytes_than_a_number_holds():
     desc.adapters = 64                                      # 2^40 in all
     assert pack() == 0 and h
     binding.lib().xgen_adapters_free(h)
+
+
+def test_attention_counts_query_rows_in_32_bits():
+    """Tiles of rows (of all query heads of a key head) are rounded up, to 128 at most."""
+    op = attention(q=64, kv=1)
+    run = lambda rows: op.run(1 << 50, 4096, batch(rows=rows, longest=rows), cache(), 1 << 55, 4096, 6 * A)      # noqa: E731
+    refused(SHAPE, run, (1 << 25) - 3)                      # 2^31 - 192
+    refused(CUDA, run, (1 << 25) - 5)                       # 2^31 - 320
