@@ -32,7 +32,8 @@
  * with a window only j > p - window.
  *   y = sum_j softmax_j( softmax_scale * <turned q, k_j> ) v_j
  * A row that sees nothing gives zeros.  Maxima and sums are fp32.  A turned query row becomes integers of 16 bits (fp32
- * layers: 24) times its largest magnitude / 32512 (8323072); their products with the codes are exact.  What is added
+ * layers: 24) times its largest magnitude / 32512 (8323072); their products with the codes are exact (fp16 layers,
+ * sequences of many rows: kept to 23 bits).  What is added
  * up is the product of a token's probability and its value scale: it has 11 bits down to 2^-20 of the row's largest one so far (fp32 layers:
  * 22 bits down to 2^-8), and is off by 2^-31 of that largest one at most below.  Pages that the row does not see have no part in it.  A
  * probability of less than 2^-100 of the row's largest may count as none.
@@ -87,7 +88,7 @@ typedef struct {
 /*
  * Make a handle.
  *   freq_host  [rotary/2] fp64, radians per position; NULL where rotary is 0.  (Kept as 64-bit fractions of a turn:
- *              angles are exact to 2^-33 of a turn at any position.)
+ *              an angle is off by some 2^-25 of a turn, at any position.)
  *   device     CUDA device ordinal, or -1 for a handle that cannot run (no CUDA call is made)
  * Errors: INVALID_ARG, UNSUPPORTED (dtype, head_dim, page_tokens, rotary), SHAPE (more than 65535 heads), ALLOC, CUDA.
  */

@@ -13,7 +13,7 @@
 // requests, 4096 features and channels, rank 16, fp16: 9.2 us (7.6 MB, 1.2 us at the memory's rate); one row 6.2 us.  Many rows
 // overlap the chains of the blocks on an SM: 4 requests of 4600 rows in all, the same sizes: rank 16 31 us, rank 64 45 us (18 us
 // for the bytes), rank 128 52 us.  With the adapters' operands in registers instead of shared memory these were 39, 55 and 90 us; with
-// clusters of eight 33, 53 and 85 us.  fp32, rank 64: 174 us, bound by the instructions that split numbers into tf32 parts (three
+// clusters of eight 33, 53 and 85 us.  fp32, rank 64: 184 us, bound by the instructions that split numbers into tf32 parts (three
 // products each: 28 TFLOP/s).
 //
 // fp16: the inner sums are brought to fp16 with a power of two for each row, so that no magnitude is lost or overflows.  fp32:
@@ -620,8 +620,10 @@ xgen_status xgen_adapters_run(const xgen_adapters_packed *h, const void *x, int6
     P.vec_x = (uintptr_t)x % 16 == 0 && x_stride * eb % 16 == 0;
     P.vec_y = ((uintptr_t)y | (uintptr_t)out) % 16 == 0 && y_stride * eb % 16 == 0 && out_stride * eb % 16 == 0;
     P.in_place = in_place;
-    // (64 requests, rank 16, of 64 rows on average: 52 us by the kernel for many rows, 40 by the other; of 96 66 and 71 us; 8 requests of
-    // 64 rows 13.4 and 9.5 us, of 96 14.2 and 12.0)
+    // us by the kernel for many rows and by the other, rank 16, lengths from a third of the longest on: 64 requests of up to 96 rows 36 and
+    // 50, of up to 144 53 and 40, of up to 300 69 and 79; 8 requests of up to 96 13.2 and 8.8, of 144 13.4 and 10.3, of 192 14.4 and 14.5;
+    // 4 of up to 300 14.1 and 11.6, of 600 18 and 22, of 2048 32 and 44.  Below some 200 rows a request neither is the faster one throughout,
+    // and an average says little of one long request among many short ones.
     const bool wide = rows / requests >= 64;
     const int64_t tiles = rows / (wide ? 64 : 16) + (requests < rows ? requests : rows);
     if (tiles > INT32_MAX / kCluster) return XGEN_ERR_SHAPE;

@@ -227,7 +227,7 @@ template <int DT, int LAY, int ITEMS> __device__ __forceinline__ void append_hea
             for (int j = 0; j < 4; ++j) {
                 uint32_t q[4];                            // 1.5 * 2^23 added leaves the nearest integer in the lowest bits
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {             // (the quotient itself: some entries lie halfway between two codes)
+                for (int k = 0; k < 4; ++k) {             // (the quotient itself, by its residual after Markstein: some entries lie halfway between two codes)
                     const float x = v[i][4 * j + k], about = x * by;
                     q[k] = __float_as_uint(fmaf(fmaf(-about, scale, x), by, about) + 12582912.0f);
                 }
@@ -1099,8 +1099,9 @@ struct Route {
 // Few rows of every sequence (with all query heads of a key head) are narrow_kernel's, in tiles of eight where that holds them, else in tiles of
 // 16.  Where a sequence may have more, wide_kernel takes those that have more than 16, and narrow_kernel is launched too unless
 // all must have.  us by narrow_kernel and by wide_kernel, four query heads to a key head, dim 128, fp16: up to 32 rows of 8
-// sequences over 8192 tokens 51 and 109, of 64 over 2000 105 and 134; up to 64 rows 77 and 89, 178 and 151, of 8 over 1024 28 and
-// 44.  (Both, each with some of the sequences, are slower than either there: 115, 166, 61.)
+// sequences over 8192 tokens 51 and 113, over 1024 28 and 72, of 64 over 2000 107 and 142; up to 64 rows 75 and 93, 30 and 47, and of 64
+// sequences over 2000, where there are tiles enough for wide_kernel, 180 and 160: the rule looks at rows alone.  (Both, each with
+// some of the sequences, are slower than either there: 115, 166, 61.)  More than kWideSequences sequences are narrow_kernel's, whatever their rows.
 static Route route_of(const xgen_attention_packed &h, const xgen_attention_batch &b) {
     const int64_t group = h.d.q_heads / h.d.kv_heads, most = (int64_t)b.longest * group;
     if (most <= 8) return {1, false};

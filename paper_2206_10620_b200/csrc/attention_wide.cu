@@ -51,12 +51,13 @@ template <int DT, int D> struct Wide {
     // The matrix unit rounds sums toward zero, and each of a unit's 8 products adds to what is lost: sums over 25 units were off by
     // 1.8e-6 on average, in one direction.  fp32 layers add up FOLD units at a time, and the totals apart: in tensor memory
     // where there is room, else in the workspace.  Root mean square errors, and us for 2 x 1024 rows over 5000 tokens, dim 128: 2.3e-6 and
-    // 495 without, 6.9e-7 and 510 by fours, 5.1e-7 and 533 by twos; dim 64 (workspace) 1.4e-6 and 304, 7.0e-7 and 329, 5.0e-7 and 367.
-    // fp16 layers 64: over 262144 tokens as one sum their values were short of two fp16 steps.  (The same sizes, dim 128: 305 without, 307.)
+    // 515 without, 6.9e-7 and 528 by fours, 5.1e-7 and 543 by twos; dim 64 (workspace) 1.4e-6 and 296, 7.0e-7 and 330, 5.0e-7 and 368.
+    // fp16 layers 64: over 262144 tokens as one sum their values were short of two fp16 steps.  (The same sizes, dim 128: 308 without, 312.)
     static constexpr bool FOLD_NEAR = TERMS * kWideUnit + 2 * D <= COLUMNS;
     static constexpr int FOLD = !SPLIT ? 64 : FOLD_NEAR ? 2 : 4;
-    // Sums of two terms lose their lowest bits, so that what is left goes into 23: an error of at most what the query row's largest component
-    // times 1/256 (1/128) of a key step gives (fp16 queries would have up to 16 steps' worth in a sum of 128).
+    // Sums of two terms lose their lowest bits, so that what is left goes into 23: at most one unit of what is left, 2^DROP/32512 of what the
+    // query row's largest component times a key step gives, and up to 0.75 of a unit, the same for a page, in the subtraction that follows:
+    // 1/145 (1/73) in all (fp16 queries would have up to 16 steps' worth in a sum of 128).
     static constexpr int DROP = D <= 128 ? 7 : 8;
     static constexpr int BLOCKS = COLUMNS == 256 && SHARED <= 104 * 1024 ? 2 : 1;
 };
