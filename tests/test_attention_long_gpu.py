@@ -77,3 +77,34 @@ def test_long_contexts_of_values_of_all_sizes(dtype, rows, copies):
         bound = bound + below_the_steps(pages, rows, one, H * G, window)
         for i in (0, copies // 2, copies - 1):
             su.close(y[i * rows:(i + 1) * rows], want, bound)
+
+
+@pytest.mark.parametrize("dtype,rows,copies,L,D,page", [
+    ("f16", 1, 256, 150_000, 32, 64), ("f16", 3, 256, 150_000, 32, 128), ("f32", 1, 256, 150_000, 32, 64),       # a piece: some 1300 units
+    ("f16", 40, 60, 30_000, 128, 64), ("f16", 40, 60, 30_000, 64, 16), ("f16", 40, 60, 30_000, 96, 32), ("f16", 40, 40, 30_000, 256, 64),
+    ("f32", 40, 60, 30_000, 64, 16)])                       # a piece: some 190 units
+@pytest.mark.parametrize("window", [0, 20_000])
+def test_sums_put_aside_at_every_place(dtype, rows, copies, L, D, page, window):
+    """So many sequences over the same pages that a block goes on with a tile for long, and that pieces begin anywhere in it; pages of small and
+    large values and of zeros, a row that is not finite: every sequence's rows are as those of one."""
+    H, G = 1, 4
+    op = binding.Attention(H * G, H, D, page, dtype, window=window)
+    pages = su.Pages([L], H, D, page, seed=D)
+    g = su.gen(6)
+    for w in range(2):
+        pages.scale[w] *= torch.exp(torch.randn(pages.scale[w].shape, device="cuda", generator=g) * (0.4 if w == 0 else 2.0))
+    pages.scale[1][pages.table[0, 100:160].long()] = 0
+    one = torch.randn((rows, H * G * D), device="cuda", generator=g).to(su.T[dtype])
+    want, bound = su.attention(pages, [rows], one, H * G, dtype, window=window)
+    bound = bound + below_the_steps(pages, rows, one, H * G, window)
+    one[-1, D:2 * D] = float("nan")
+    want[-1, D:2 * D] = float("nan")
+    q = one.repeat(copies, 1)
+    start, length = su.starts([rows] * copies), su.ints([L] * copies)
+    table = pages.table.expand(copies, -1).contiguous()
+    batch = binding.Batch(copies, rows * copies, rows, start.data_ptr(), length.data_ptr(), table.data_ptr(), table.shape[1])
+    y = torch.zeros_like(q)
+    work = torch.full((op.workspace(batch) // 4 + 1,), float("nan"), device="cuda")
+    op.run(q.data_ptr(), H * G * D, batch, pages.handle, y.data_ptr(), H * G * D, work.data_ptr(), su.stream())
+    op.sync(su.stream())
+    su.close(y, want.repeat(copies, 1), bound.repeat(copies, 1))

@@ -27,9 +27,9 @@ def tight(dtype, lengths, n, H, G, D, page, edit, window=0, seed=0):
 @pytest.mark.parametrize("dtype", ["f32", "f16"])
 @pytest.mark.parametrize("D", [32, 128, 256])
 @pytest.mark.parametrize("n", [1, 5, 40, 150])
-@pytest.mark.parametrize("size", [2.0 ** -126, 1e-37, 1e-30])
+@pytest.mark.parametrize("size", [1e-40, 2.0 ** -126, 1e-37, 1e-30])
 def test_tiny_values(dtype, D, n, size):
-    """Value scales down to the least that appending makes, in all pages, and in the first ones, larger ones behind them."""
+    """Value scales down to the least that appending makes, and below, in all pages, and in the first ones, larger ones behind them."""
     def alone(pages, q):
         pages.scale[1].fill_(size)
 
@@ -73,15 +73,12 @@ def test_the_weight_on_the_small_values(dtype, n, ratio, low):
         check(dtype, [400, 150], [n, min(n, 150)], H, G, D, page, rotary=0, edit=edit)
 
 
-@pytest.mark.parametrize("dtype", ["f32", "f16"])
 @pytest.mark.parametrize("n", [8, 16, 100, 140])
-@pytest.mark.parametrize("ratio", [1e4, 1e6, 1e9, 1e14, 1e30])
+@pytest.mark.parametrize("dtype,ratio", [("f16", 1e4), ("f32", 1e4), ("f32", 1e6), ("f32", 1e9), ("f32", 1e14), ("f32", 1e30)])      # (results within fp16)
 @pytest.mark.parametrize("window", [0, 96])
 def test_pages_that_a_row_does_not_see(dtype, n, ratio, window):
     """Large values behind a row, or before its window, in steps that other rows see: the row is as exact as without them."""
     H, G, D, page, L = 1, 2, 64, 16, 304
-    if dtype == "f16" and ratio > 1e4:
-        pytest.skip("beyond fp16")                          # (values of up to 3 times the ratio)
     op, freq = make(H, D, page, dtype, rotary=0, q_heads=H * G, window=window)
     pages = su.Pages([L], H, D, page, seed=5)
     q = torch.randn((n, H * G * D), device="cuda", generator=su.gen(6)).to(su.T[dtype])
